@@ -54,10 +54,14 @@ typedef enum {
     MOE_ERR_HIP = 4            /* a HIP call or kernel launch failed                */
 } moe_status;
 
-typedef enum { MOE_F32 = 0, MOE_BF16 = 1 } moe_dtype;
+typedef enum { MOE_F32 = 0, MOE_BF16 = 1,
+               MOE_E4M3 = 2     /* 8 bits (OCP e4m3: 3 bits of mantissa, largest value 448, no infinities): moe_quant_* only */
+} moe_dtype;
 
 /* trailing activation of an expert's first linear layer (Section 3.4: "ReLU or GeLU") */
-typedef enum { MOE_ACT_RELU = 0, MOE_ACT_GELU = 1 } moe_activation;
+typedef enum { MOE_ACT_RELU = 0, MOE_ACT_GELU = 1,
+               MOE_ACT_NONE = -1    /* moe_quant_* only */
+} moe_activation;
 
 typedef struct {
     int32_t T, d_model, d_ff, E, k;
@@ -311,6 +315,88 @@ size_t moe_noalloc_max_workspace(void);     /* = MOE_NOALLOC_MAX_WORKSPACE */
 moe_status moe_layer_forward_noalloc(const moe_shape* shape, const void* x, const void* w_gate,
                                      const float* gate_bias, const void* w1, const void* w2,
                                      const uint8_t* mask, int32_t H, void* out, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * 8-bit layers.  A cold expert costs its parameter bytes (Section 3.1), so parameters of half the size are half the
+ * time, and hot experts run at twice the matrix rate.  The calls below take the layer from the residual stream to the
+ * experts' rows in e4m3: the norm in front of the layer with a quantised output, and linear layers on quantised rows and
+ * weights, for one weight matrix and grouped by expert.  moe_route, moe_permute (with x_perm NULL) and moe_combine are
+ * the steps between and after them.
+ *
+ * Quantised rows [R, C]: e4m3 codes in rows of moe_quant_pitch(C) bytes (C rounded up to 128; the codes past C are zero) and
+ * fp32 scales [R, ceil(C / 128)]; value (r, c) is code(r, c) * scale(r, c / 128).  As these calls write them, a block of 128
+ * values (a row's last block may be shorter) has scale = max(max |v| / 448, 2^-126) and code = v / scale rounded to the nearest
+ * e4m3 value, ties to even; a block that holds a NaN or an infinity has a NaN for its scale and NaN codes, so that it is NaN
+ * throughout.  The products take any scales.
+ * Quantised weights of E matrices [N, K] ("out-features x in-features"): scales [E, ceil(N / 128), ceil(K / 128)], one for every
+ * 128 x 128 block, and the codes in the products' layout, made once by moe_quantize_weights.
+ * Codes and packed weights are 16-byte aligned, other pointers to the size of their elements.
+ */
+#define MOE_QUANT_BLOCK 128
+
+/* Bytes of a quantised row of n values; 0 if n < 1. */
+size_t moe_quant_pitch(int32_t n);
+
+/* Bytes of E packed weight matrices [N, K]; 0 on sizes that moe_quantize_weights refuses. */
+size_t moe_quant_weight_bytes(int32_t E, int32_t N, int32_t K);
+
+/*
+ * One-time weight preparation.  src [E, N, K], row-major, of type src_dtype:
+ *   MOE_F32, MOE_BF16: quantised; `scales` [E, ceil(N/128), ceil(K/128)] is written by the rule above, with the block of 128 x 128.
+ *   MOE_E4M3: a checkpoint's own codes, laid out as they are; their scales are the caller's and `scales` is not used (NULL).
+ * dst (moe_quant_weight_bytes bytes): for each matrix fragments of 16 rows x 128 columns, fragment (nb, kb) at byte
+ *   ((nb * ceil(K/128)) + kb) * 2048, nb < 8 * ceil(N/128); inside a fragment the 16 bytes of row r = l % 16 from column
+ *   64 * h + 16 * (l / 16) on sit at h * 1024 + 16 * l, l = 0..63, h = 0, 1 (two loads of 16 bytes per wavefront lane).
+ *   Rows past N and columns past K are zero.
+ * src and dst must not overlap.  1 <= E <= 1024, 1 <= N, K <= 2^24.
+ */
+moe_status moe_quantize_weights(int32_t E, int32_t N, int32_t K, int32_t src_dtype, const void* src, void* dst, float* scales,
+                                void* stream);
+
+/*
+ * The norm in front of a layer, with the residual's addition and a quantised output:
+ *   s = x + residual, rounded once to dtype (x itself where residual is NULL);
+ *   n[r, c] = s[r, c] / sqrt(mean_c(s[r, c]^2) + eps) * weight[c]   (weight NULL: ones), in fp32, squares summed in fp32;
+ *   sum_out  [rows, d] (dtype) = s, or NULL: the residual stream that the next layer continues;
+ *   norm_out [rows, d] (dtype) = n rounded once, or NULL: what moe_route reads;
+ *   q, q_scales: n as quantised rows [rows, d].
+ * x, residual [rows, d] of dtype MOE_F32 or MOE_BF16, weight [d] fp32.  sum_out may be x or residual itself; no other buffers overlap.
+ * rows >= 0 (0: a no-op), 1 <= d <= 2^24, eps >= 0 and finite.
+ */
+moe_status moe_norm_quantize(int32_t rows, int32_t d, int32_t dtype, const void* x, const void* residual, const float* weight, float eps,
+                             void* sum_out, void* norm_out, void* q, float* q_scales, void* stream);
+
+/* A product on quantised rows: `rows` rows of N outputs from rows of K. */
+typedef struct {
+    int32_t rows, N, K;
+    int32_t E;            /* weight matrices; 1 for moe_quant_linear                                    */
+    int32_t k;            /* with a `perm`: assignments per token, rows % k == 0 (else 1)                */
+    int32_t activation;   /* moe_activation                                                             */
+    int32_t out_dtype;    /* MOE_F32, MOE_BF16: [rows, N], last index contiguous; MOE_E4M3: quantised rows */
+} moe_quant_shape;
+
+/* Bytes of workspace of the two calls below (0 on a shape that they refuse). */
+size_t moe_quant_workspace_bytes(const moe_quant_shape* shape);
+
+/*
+ * out[r, n] = act( sum_b sa[r, b] * sw[n/128, b] * sum_{c in block b} a[r, c] * w[n, c] + bias[n] )
+ * a, sa: quantised rows [rows, K]; w, sw: packed weights and their scales (E = 1); bias [N] fp32 or NULL.  Code products and sums are
+ * accumulated in fp32 and the result is rounded once, to out_dtype.  out_scales: scales of the quantised output, NULL for the
+ * other types.  ws: at least moe_quant_workspace_bytes, 256-byte aligned.  Outputs overlap nothing.
+ */
+moe_status moe_quant_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const void* w, const float* w_scales,
+                            const float* bias, void* out, float* out_scales, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * The same for E weight matrices and rows grouped by expert: rows offsets[e] .. offsets[e+1] (device, as moe_route writes them)
+ * are products with matrix e, bias [E, N].  perm NULL: row p reads quantised row p of [rows, K].  perm [rows] (as moe_permute writes
+ * it): row p reads quantised row perm[p] / k of [rows / k, K], the token's.  mask [E] or NULL: rows of experts with mask[e] == 0 are
+ * neither computed nor written.  Offsets and perm are read on the device and clamped to the buffers' sizes, so that wrong ones give
+ * wrong rows but no access outside.
+ */
+moe_status moe_quant_expert_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const int32_t* perm,
+                                   const int32_t* offsets, const uint8_t* mask, const void* w, const float* w_scales, const float* bias,
+                                   void* out, float* out_scales, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

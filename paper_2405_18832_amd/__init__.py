@@ -17,7 +17,9 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("MOE_FFN_LIB") or os.path.join(_PKG, "libmoe_ffn_gfx950.so")
 
 MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP = range(5)
-MOE_F32, MOE_BF16 = 0, 1
+MOE_F32, MOE_BF16, MOE_E4M3 = 0, 1, 2
+MOE_ACT_NONE, MOE_ACT_RELU, MOE_ACT_GELU = -1, 0, 1
+MOE_QUANT_BLOCK = 128
 MOE_MAX_K, MOE_MAX_E = 8, 1024
 
 EXPORTS = ["moe_init", "moe_noalloc_max_workspace", "moe_layer_forward_noalloc",
@@ -25,7 +27,9 @@ EXPORTS = ["moe_init", "moe_noalloc_max_workspace", "moe_layer_forward_noalloc",
            "moe_set_profile_events", "moe_tiled_kernel_min_rows",
            "moe_parameter_movement_bytes", "moe_activation_movement_bytes", "moe_plan_devices", "moe_fetch_experts", "moe_tune_alpha",
            "moe_route", "moe_select_hot", "moe_permute", "moe_expert_ffn", "moe_expert_ffn_biased", "moe_combine",
-           "moe_layer_forward", "moe_layer_forward_biased"]
+           "moe_layer_forward", "moe_layer_forward_biased",
+           "moe_quant_pitch", "moe_quant_weight_bytes", "moe_quantize_weights", "moe_norm_quantize", "moe_quant_workspace_bytes",
+           "moe_quant_linear", "moe_quant_expert_linear"]
 
 
 class MoEError(RuntimeError):
@@ -37,6 +41,10 @@ class MoEError(RuntimeError):
 class moe_shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("T", "d_model", "d_ff", "E", "k", "dtype", "renormalize", "activation")]
+
+
+class moe_quant_shape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "N", "K", "E", "k", "activation", "out_dtype")]
 
 
 _lib = None
@@ -101,6 +109,21 @@ def load() -> ctypes.CDLL:
     lib.moe_combine.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp]
     lib.moe_layer_forward.restype = ctypes.c_int
     lib.moe_layer_forward.argtypes = [sp, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    qp = ctypes.POINTER(moe_quant_shape)
+    lib.moe_quant_pitch.argtypes = [i32]
+    lib.moe_quant_pitch.restype = sz
+    lib.moe_quant_weight_bytes.argtypes = [i32, i32, i32]
+    lib.moe_quant_weight_bytes.restype = sz
+    lib.moe_quantize_weights.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.moe_quantize_weights.restype = ctypes.c_int
+    lib.moe_norm_quantize.argtypes = [i32, i32, i32, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.moe_norm_quantize.restype = ctypes.c_int
+    lib.moe_quant_workspace_bytes.argtypes = [qp]
+    lib.moe_quant_workspace_bytes.restype = sz
+    lib.moe_quant_linear.argtypes = [qp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_quant_linear.restype = ctypes.c_int
+    lib.moe_quant_expert_linear.argtypes = [qp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_quant_expert_linear.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -114,6 +137,16 @@ def make_shape(T, d_model, d_ff, E, k, dtype, renormalize, activation=0) -> moe_
         dtype = {"f32": MOE_F32, "bf16": MOE_BF16}[dtype]
     return moe_shape(int(T), int(d_model), int(d_ff), int(E), int(k), int(dtype),
                      int(bool(renormalize)), int(activation))
+
+
+_DTYPE_NAMES = {"f32": MOE_F32, "bf16": MOE_BF16, "e4m3": MOE_E4M3}
+_ACT_NAMES = {"none": MOE_ACT_NONE, "relu": MOE_ACT_RELU, "gelu": MOE_ACT_GELU}
+
+
+def make_quant_shape(rows, N, K, E=1, k=1, activation="none", out_dtype="bf16") -> moe_quant_shape:
+    """`activation`: "none" | "relu" | "gelu", `out_dtype`: "f32" | "bf16" | "e4m3" (or the C values)."""
+    return moe_quant_shape(int(rows), int(N), int(K), int(E), int(k), int(_ACT_NAMES.get(activation, activation)),
+                           int(_DTYPE_NAMES.get(out_dtype, out_dtype)))
 
 
 def _ptr(t) -> Optional[int]:
@@ -285,3 +318,39 @@ def moe_layer_forward(shape, x, w_gate, gate_bias, w1, w2, mask, H, out, topk_id
                                     _ptr(w2), _ptr(mask), int(H), _ptr(out), _ptr(topk_idx), _ptr(topk_w),
                                     _ptr(counts), _ptr(perm), _ptr(hot_mask_out), _ptr(ws), _nbytes(ws),
                                     _stream(stream)), "moe_layer_forward")
+
+
+# ---- 8-bit layers --------------------------------------------------------------------------------------------------
+# Quantised rows and packed weights are one-byte tensors (torch.float8_e4m3fn or torch.uint8).
+def moe_quant_pitch(n) -> int:
+    return int(load().moe_quant_pitch(int(n)))
+
+
+def moe_quant_weight_bytes(E, N, K) -> int:
+    return int(load().moe_quant_weight_bytes(int(E), int(N), int(K)))
+
+
+def moe_quantize_weights(E, N, K, src_dtype, src, dst, scales, stream=None) -> None:
+    _check(load().moe_quantize_weights(int(E), int(N), int(K), int(_DTYPE_NAMES.get(src_dtype, src_dtype)), _ptr(src), _ptr(dst),
+                                       _ptr(scales), _stream(stream)), "moe_quantize_weights")
+
+
+def moe_norm_quantize(rows, d, dtype, x, residual, weight, eps, sum_out, norm_out, q, q_scales, stream=None) -> None:
+    _check(load().moe_norm_quantize(int(rows), int(d), int(_DTYPE_NAMES.get(dtype, dtype)), _ptr(x), _ptr(residual), _ptr(weight),
+                                    float(eps), _ptr(sum_out), _ptr(norm_out), _ptr(q), _ptr(q_scales), _stream(stream)),
+           "moe_norm_quantize")
+
+
+def moe_quant_workspace_bytes(shape: moe_quant_shape) -> int:
+    return int(load().moe_quant_workspace_bytes(ctypes.byref(shape)))
+
+
+def moe_quant_linear(shape, a, a_scales, w, w_scales, bias, out, out_scales, ws, stream=None) -> None:
+    _check(load().moe_quant_linear(ctypes.byref(shape), _ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(out),
+                                   _ptr(out_scales), _ptr(ws), _nbytes(ws), _stream(stream)), "moe_quant_linear")
+
+
+def moe_quant_expert_linear(shape, a, a_scales, perm, offsets, mask, w, w_scales, bias, out, out_scales, ws, stream=None) -> None:
+    _check(load().moe_quant_expert_linear(ctypes.byref(shape), _ptr(a), _ptr(a_scales), _ptr(perm), _ptr(offsets), _ptr(mask),
+                                          _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(out), _ptr(out_scales), _ptr(ws), _nbytes(ws),
+                                          _stream(stream)), "moe_quant_expert_linear")

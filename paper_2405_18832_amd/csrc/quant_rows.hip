@@ -1,0 +1,285 @@
+// Quantised rows and weights: the RMS norm in front of a layer with the residual's addition, and the weights' layout.
+#include <type_traits>
+
+#include "quant.hpp"
+
+namespace moe {
+
+// ---- moe_norm_quantize ----------------------------------------------------------------------------------------------
+// One pass over the data: the row is read once (x, residual), kept in registers as fp32, its squares are summed, and sum, norm and
+// codes are written from the registers.  Bound by memory: per value 2 or 4 + 4 bytes in, 1 to 9 out.
+//
+// A lane holds chunks of 8 consecutive values, so that 16 lanes are a block of 128 (its maximum takes four DPP rotations) and a
+// wavefront covers 512 values per chunk; chunk c of a row is done by wavefront c % WPR of the row's WPR wavefronts.
+
+template <typename ST> struct Eight;
+template <> struct Eight<uint16_t> {
+    static __device__ __forceinline__ void load(const uint16_t* p, float (&v)[8]) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[8]) {
+        *reinterpret_cast<uint4*>(p) =
+            uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    }
+    static __device__ __forceinline__ float round(float v) { return bf16_to_f32(f32_to_bf16(v)); }
+};
+template <> struct Eight<float> {
+    static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
+        const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            v[i] = a[i];
+            v[4 + i] = b[i];
+        }
+    }
+    static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
+        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    }
+    static __device__ __forceinline__ float round(float v) { return v; }
+};
+
+// 8 values from column `c` of a row of d; those past the end are zero.  VEC: whole chunks only, 16-byte aligned.
+template <typename ST, bool VEC>
+__device__ __forceinline__ void load8(const ST* row, int c, int d, float (&v)[8]) {
+    if constexpr (VEC) {
+        if (c < d) {
+            Eight<ST>::load(row + c, v);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = 0.f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = c + i < d ? Storage<ST>::load(row + c + i) : 0.f;
+    }
+}
+template <typename ST, bool VEC>
+__device__ __forceinline__ void store8(ST* row, int c, int d, const float (&v)[8]) {
+    if constexpr (VEC) {
+        if (c < d) Eight<ST>::store(row + c, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (c + i < d) Storage<ST>::store(row + c + i, v[i]);
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+constexpr int kNormWaves = 4;               // wavefronts of a block
+constexpr int kNormValues = 512;            // values of a wavefront's chunk
+
+struct NormArgs {
+    const void *x, *residual;
+    const float* weight;
+    float eps;
+    void *sum_out, *norm_out;
+    uint8_t* q;
+    float* q_scales;
+    int rows, d;
+};
+
+// NV: chunks that a wavefront keeps in registers; 0: rows longer than any variant keeps, which are read a second time.
+template <typename ST, int WPR, int NV, bool VEC>
+__global__ __launch_bounds__(kNormWaves * 64) void norm_quantize_kernel(const NormArgs a) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int part = wave % WPR;
+    const int row = blockIdx.x * (kNormWaves / WPR) + wave / WPR;
+    const bool live = row < a.rows;                         // the block meets at a barrier below
+    const int d = a.d;
+    const size_t at = static_cast<size_t>(live ? row : 0) * d;
+    const ST* x = static_cast<const ST*>(a.x) + at;
+    const ST* res = a.residual ? static_cast<const ST*>(a.residual) + at : nullptr;
+    ST* sum_out = a.sum_out ? static_cast<ST*>(a.sum_out) + at : nullptr;
+    ST* norm_out = a.norm_out ? static_cast<ST*>(a.norm_out) + at : nullptr;
+    const size_t pitch = quant_pitch(d);
+    uint8_t* q = a.q + static_cast<size_t>(live ? row : 0) * pitch;
+    float* q_scales = a.q_scales + static_cast<size_t>(live ? row : 0) * (pitch / kQuantBlock);
+    const int chunks = (static_cast<int>(pitch) + kNormValues - 1) / kNormValues;
+    auto column = [&](int chunk) { return chunk * kNormValues + lane * 8; };
+    auto read_sum = [&](int chunk, float (&s)[8]) {
+        load8<ST, VEC>(x, column(chunk), d, s);
+        if (res != nullptr) {
+            float r[8];
+            load8<ST, VEC>(res, column(chunk), d, r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = Eight<ST>::round(s[i] + r[i]);
+        }
+    };
+
+    float kept[NV > 0 ? NV : 1][8];
+    float squares = 0.f;
+    if (live) {
+        if constexpr (NV > 0) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+                if (j * WPR + part < chunks) {
+                    read_sum(j * WPR + part, kept[j]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) kept[j][i] = 0.f;
+                }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float p = 0.f;                              // short chains: the rounding error of a sum grows with its length
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p = fmaf(kept[j][i], kept[j][i], p);
+                squares += p;
+            }
+        } else {
+            for (int c = part; c < chunks; c += WPR) {
+                read_sum(c, kept[0]);
+                float p = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p = fmaf(kept[0][i], kept[0][i], p);
+                squares += p;
+            }
+        }
+    }
+    squares = wave_sum(squares);
+    if constexpr (WPR > 1) {
+        __shared__ float parts[kNormWaves];
+        if (lane == 0) parts[wave] = squares;
+        __syncthreads();
+        squares = 0.f;
+#pragma unroll
+        for (int w = 0; w < WPR; ++w) squares += parts[wave / WPR * WPR + w];
+    }
+    if (!live) return;
+    const float rho = 1.f / sqrtf(squares / static_cast<float>(d) + a.eps);
+
+    auto finish = [&](int chunk, float (&s)[8]) {
+        const int c = column(chunk);
+        if (sum_out != nullptr) store8<ST, VEC>(sum_out, c, d, s);
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] *= rho;
+        if (a.weight != nullptr) {
+            float w[8];
+            load8<float, VEC>(a.weight, c, d, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] *= w[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) most = max(most, c + i < d ? magnitude(s[i]) : 0u);
+        if (norm_out != nullptr) store8<ST, VEC>(norm_out, c, d, s);
+        most = row16_max(most);
+        const float scale = block_scale(most), inv = 1.f / scale;
+        if (c < static_cast<int>(pitch)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) s[i] = c + i < d ? s[i] * inv : 0.f;    // zeros past the end, also where the scale is NaN
+            const uint2 codes = uint2{pack_e4m3x4(s[0], s[1], s[2], s[3]), pack_e4m3x4(s[4], s[5], s[6], s[7])};
+            *reinterpret_cast<uint2*>(q + c) = codes;
+            if ((lane & 15) == 0) q_scales[c / kQuantBlock] = scale;
+        }
+    };
+    if constexpr (NV > 0) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            if (j * WPR + part < chunks) finish(j * WPR + part, kept[j]);
+    } else {
+        for (int c = part; c < chunks; c += WPR) {
+            read_sum(c, kept[0]);
+            finish(c, kept[0]);
+        }
+    }
+}
+
+template <typename ST, bool VEC>
+static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
+    const int chunks = static_cast<int>((quant_pitch(a.d) + kNormValues - 1) / kNormValues);
+    const dim3 block(kNormWaves * 64);
+    auto go = [&](auto kernel, int wpr) {
+        const int per_block = kNormWaves / wpr;
+        kernel<<<dim3((a.rows + per_block - 1) / per_block), block, 0, stream>>>(a);
+    };
+    if (chunks <= kNormWaves) go(norm_quantize_kernel<ST, 4, 1, VEC>, 4);
+    else if (chunks <= 2 * kNormWaves) go(norm_quantize_kernel<ST, 4, 2, VEC>, 4);
+    else if (chunks <= 8 * kNormWaves) go(norm_quantize_kernel<ST, 4, 8, VEC>, 4);
+    else go(norm_quantize_kernel<ST, 4, 0, VEC>, 4);
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_quantize(int rows, int d, int dtype, const void* x, const void* residual, const float* weight, float eps,
+                                void* sum_out, void* norm_out, uint8_t* q, float* q_scales, hipStream_t stream) {
+    const NormArgs a{x, residual, weight, eps, sum_out, norm_out, q, q_scales, rows, d};
+    uintptr_t all = 0;
+    for (const void* p : {x, residual, static_cast<const void*>(weight), static_cast<const void*>(sum_out), static_cast<const void*>(norm_out)})
+        all |= reinterpret_cast<uintptr_t>(p);
+    const bool vec = d % 8 == 0 && all % 16 == 0;
+    if (dtype == MOE_BF16) return vec ? launch_norm<uint16_t, true>(a, stream) : launch_norm<uint16_t, false>(a, stream);
+    return vec ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
+}
+
+// ---- moe_quantize_weights -------------------------------------------------------------------------------------------
+// A block of threads per 128 x 128 block of a matrix.  Thread t holds 64 columns of row t / 2: the block's maximum, then the codes, as
+// four pieces of 16 bytes at the places that the products' loads want them (moe.h).
+template <typename ST>      // float, uint16_t (bf16) or uint8_t (codes)
+__global__ __launch_bounds__(256) void quantize_weights_kernel(const ST* __restrict__ src, uint8_t* __restrict__ dst,
+                                                               float* __restrict__ scales, int N, int K) {
+    const int kb = blockIdx.x, nb = blockIdx.y, e = blockIdx.z;
+    const int kblocks = gridDim.x, nblocks = gridDim.y;
+    const int r = threadIdx.x >> 1, half = threadIdx.x & 1;
+    const int n = nb * kQuantBlock + r, k0 = kb * kQuantBlock + half * 64;
+    const ST* row = src + (static_cast<size_t>(e) * N + min(n, N - 1)) * K;
+    uint32_t codes[16];
+    if constexpr (std::is_same_v<ST, uint8_t>) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            codes[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n < N && k0 + 4 * i + j < K) codes[i] |= static_cast<uint32_t>(row[k0 + 4 * i + j]) << (8 * j);
+        }
+    } else {
+        float v[64];
+        uint32_t most = 0;
+#pragma unroll
+        for (int i = 0; i < 64; ++i) {
+            v[i] = n < N && k0 + i < K ? Storage<ST>::load(row + k0 + i) : 0.f;
+            most = max(most, magnitude(v[i]));
+        }
+        __shared__ uint32_t all[4];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), o, 64)));
+        if ((threadIdx.x & 63) == 0) all[threadIdx.x >> 6] = most;
+        __syncthreads();
+        most = max(max(all[0], all[1]), max(all[2], all[3]));
+        const float scale = block_scale(most), inv = 1.f / scale;
+        if (threadIdx.x == 0) scales[(static_cast<size_t>(e) * nblocks + nb) * kblocks + kb] = scale;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            // columns and rows past the end stay zero in a block whose scale is NaN
+            codes[i] = pack_e4m3x4(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (n >= N || k0 + 4 * i + j >= K) codes[i] &= ~(0xffu << (8 * j));
+        }
+    }
+    uint8_t* frag = dst + ((static_cast<size_t>(e) * nblocks * 8 + nb * 8 + (r >> 4)) * kblocks + kb) * kFragBytes;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint4*>(frag + half * 1024 + (g * 16 + (r & 15)) * 16) =
+            uint4{codes[4 * g], codes[4 * g + 1], codes[4 * g + 2], codes[4 * g + 3]};
+}
+
+hipError_t launch_quantize_weights(int E, int N, int K, int src_dtype, const void* src, uint8_t* dst, float* scales, hipStream_t stream) {
+    const dim3 grid(quant_blocks(K), quant_blocks(N), E), block(256);
+    if (src_dtype == MOE_F32) quantize_weights_kernel<<<grid, block, 0, stream>>>(static_cast<const float*>(src), dst, scales, N, K);
+    else if (src_dtype == MOE_BF16) quantize_weights_kernel<<<grid, block, 0, stream>>>(static_cast<const uint16_t*>(src), dst, scales, N, K);
+    else quantize_weights_kernel<<<grid, block, 0, stream>>>(static_cast<const uint8_t*>(src), dst, scales, N, K);
+    return hipGetLastError();
+}
+
+}  // namespace moe
