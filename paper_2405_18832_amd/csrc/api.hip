@@ -69,6 +69,7 @@ hipError_t ensure_ready() {
     if ((e = configure_tile_kernels(dev)) != hipSuccess) return e;
     if ((e = configure_f32_kernels()) != hipSuccess) return e;
     if ((e = configure_route_kernels(dev)) != hipSuccess) return e;
+    if ((e = configure_quant_kernels()) != hipSuccess) return e;
     // this device's copy of the scratch array (each GPU has its own, at its own address)
     void* p = nullptr;
     if ((e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch))) != hipSuccess) return e;

@@ -496,5 +496,6 @@ hipError_t configure_ffn_kernels(int dev);       // ffn.hip
 hipError_t configure_tile_kernels(int dev);      // ffn_tile.hip
 hipError_t configure_f32_kernels();              // ffn_f32.hip
 hipError_t configure_route_kernels(int dev);     // route.hip
+hipError_t configure_quant_kernels();            // quant_linear.hip
 
 }  // namespace moe

@@ -5,6 +5,7 @@
 // A product of codes starts from zero in every block of 128 columns and is added to the fp32 accumulators by one multiply-add per
 // value, scaled with the block's two scales: the weights' is the same for the whole wavefront, the rows' one value per lane, because
 // the weights are the matrix instruction's first operand and a lane's results are four columns of one row.
+#include <algorithm>
 #include <type_traits>
 
 #include "quant.hpp"
@@ -367,16 +368,170 @@ __global__ __launch_bounds__(64 * WN * KS) void quant_stream_kernel(const QuantA
     }
 }
 
+// ---- many rows per matrix: tiles in LDS -----------------------------------------------------------------------------
+// Unit: 256 rows x 128 columns by 8 wavefronts (4 x 2, 64 x 64 each), a block of 128 columns of the contraction per step, through a
+// ring of three LDS stages: one being read, one that has landed (its first fragments are read ahead), one in flight.  Everything goes from
+// memory to LDS directly, 16 bytes per lane; a stage holds
+//   rows     [256][128 bytes], copied a whole line per eight lanes; the 16-byte pieces of a row are permuted by its number so that the
+//            operand reads (16 rows x one piece) meet no bank twice: piece c of row r lies at c ^ (r / 2 % 8)
+//   weights  8 fragments of 2 KiB as they are packed, 16 rows each
+//   scales   of the 256 rows, and the weights' (one for the unit's 128 columns)
+constexpr int kTileRows = 256, kTileCols = kQuantBlock, kTileWaves = 8, kTileStages = 3;
+constexpr int kStageW = kTileRows * kQuantBlock, kStageS = kStageW + kTileCols * kQuantBlock, kStage = kStageS + kTileRows * 4 + 256;
+constexpr int kTileMost = kTileStages * kStage, kTileStarts = kTileMost + 2 * kTileRows * 4;
+constexpr int kTileLdsBytes = kTileStarts + (MOE_MAX_E + 1 + kTileWaves) * 4;
+static_assert(kTileLdsBytes <= 160 * 1024, "fits a CU");
+
+// 4 bytes per lane into LDS, as copy16_to_lds
+__device__ __forceinline__ void copy4_to_lds(const void* src, uint32_t lds_base) {
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(dst) : "memory");
+}
+
+template <int OUT>
+__global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const QuantArgs a, int min_rows) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kTileMost);           // [2][256]
+    int32_t* starts = reinterpret_cast<int32_t*>(smem + kTileStarts);
+    count_tiles<kTileWaves * 64>(a, kTileRows, min_rows, a.rows, starts, starts + MOE_MAX_E + 1);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wm = wave >> 1, wn = wave & 1;
+    const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
+    const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
+    const int units = starts[a.E] * groups;
+    const uint32_t lds = lds_address(smem);
+    // copies: wavefront w brings rows 32 w ... 32 w + 31, weight fragment w, and the scales of rows 64 (w % 4) ... or of the weights
+    const uint32_t to_rows = lds + wave * 4096, to_weights = lds + kStageW + wave * 2048;
+    const uint32_t to_scales = lds + kStageS + (wave < 4 ? wave * 256 : kTileRows * 4);
+    // operand reads: piece g of row r, the other half's piece 4 + g is 64 bytes away by exclusive or
+    const int at_x = (wm * 64 + r) * kQuantBlock + ((g ^ (r >> 1)) << 4), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
+    const int at_sx = kStageS + (wm * 64 + r) * 4, at_sw = kStageS + kTileRows * 4;
+
+    for (int u = xcd_position(); u < units; u += gridDim.x) {
+        const int e = __builtin_amdgcn_readfirstlane(expert_of(starts, a.E, u / groups));
+        const int tiles = starts[e + 1] - starts[e], local = u - starts[e] * groups;
+        // eight column groups of a tile, then the next tile's: 32 neighbours share four tiles' rows and eight groups' weights
+        const int band = local / (tiles * 8), width = min(8, groups - band * 8), rest = local - band * tiles * 8;
+        const int tile = rest / width, group = band * 8 + rest % width;
+        const Segment seg = segment_of(a, e);
+        const int row0 = __builtin_amdgcn_readfirstlane(seg.row0 + tile * kTileRows);
+        const int rows = __builtin_amdgcn_readfirstlane(min(kTileRows, seg.rows - tile * kTileRows));
+        const int n0 = group * kTileCols;
+
+        const uint8_t* from_rows[4];
+        const uint8_t* from_weights = a.w + static_cast<size_t>(e) * quant_matrix_bytes(a.N, a.K) +
+                                      static_cast<size_t>(n0 / 16 + wave) * KB * kFragBytes + lane * 16;
+        const float* from_scales;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int in_tile = wave * 32 + i * 8 + (lane >> 3);
+            const size_t row = source_row(a, row0 + min(in_tile, rows - 1));
+            from_rows[i] = a.a + row * pitch + (((lane & 7) ^ (in_tile >> 1 & 7)) << 4);
+        }
+        if (wave < 4) from_scales = a.a_scales + static_cast<size_t>(source_row(a, row0 + min(wave * 64 + lane, rows - 1))) * KB;
+        else from_scales = a.w_scales + (static_cast<size_t>(e) * groups + group) * KB;
+        auto stage_in = [&](int slot) {
+            const int at = slot * kStage;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                copy16_to_lds(from_rows[i], to_rows + at + i * 1024);
+                from_rows[i] += kQuantBlock;
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) copy16_to_lds(from_weights + i * 1024, to_weights + at + i * 1024);
+            from_weights += kFragBytes;
+            copy4_to_lds(from_scales, to_scales + at);
+            ++from_scales;
+        };
+        f32x4 acc[4][4];
+#pragma unroll
+        for (int nf = 0; nf < 4; ++nf)
+#pragma unroll
+            for (int tf = 0; tf < 4; ++tf) acc[nf][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the ring is free
+        stage_in(0);
+        if (KB > 1) stage_in(1);
+        if (KB > 1) asm volatile("s_waitcnt vmcnt(7)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        auto read_codes = [&](const unsigned char* p, int other) {
+            const i32x4 lo = *reinterpret_cast<const i32x4*>(p), hi = *reinterpret_cast<const i32x4*>(p + other);
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        const int x_other = (at_x & 64) ? -64 : 64;
+        Widened w[4];
+#pragma unroll
+        for (int nf = 0; nf < 4; ++nf) w[nf] = widen(read_codes(smem + at_w + nf * kFragBytes, 1024));
+        i32x8 x = read_codes(smem + at_x, x_other);
+        int slot = 0;
+        for (int j = 0; j < KB; ++j) {
+            const int next = slot == kTileStages - 1 ? 0 : slot + 1, after = next == kTileStages - 1 ? 0 : next + 1;
+            const unsigned char* st = smem + slot * kStage;
+            const unsigned char* st_next = smem + next * kStage;
+            const bool more = j + 1 < KB;
+            if (more) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (j + 2 < KB) stage_in(after);
+            const float sw = *reinterpret_cast<const float*>(st + at_sw);
+#pragma unroll
+            for (int tf = 0; tf < 4; ++tf) {
+                const float scale = *reinterpret_cast<const float*>(st + at_sx + tf * 64) * sw;
+                const Widened wx = widen(x);
+                if (tf < 3) x = read_codes(st + at_x + (tf + 1) * kFragBytes, x_other);
+                else if (more) x = read_codes(st_next + at_x, x_other);
+#pragma unroll
+                for (int nf = 0; nf < 4; ++nf) {
+                    const f32x4 p = mfma_block(w[nf], wx);
+                    if (tf == 3 && more) w[nf] = widen(read_codes(st_next + at_w + nf * kFragBytes, 1024));
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[nf][tf][i] = fmaf(scale, p[i], acc[nf][tf][i]);
+                }
+            }
+            slot = next;
+        }
+        const int col0 = n0 + wn * 64, first = wm * 64;            // this wavefront's columns and rows
+        finish_values(a, e, col0, acc);
+        if constexpr (OUT == kOutE4m3) {
+            uint32_t most[4];
+            row_magnitudes(a.N, col0, acc, most);
+            if (lane < 16) {
+#pragma unroll
+                for (int tf = 0; tf < 4; ++tf) mosts[wn * kTileRows + first + tf * 16 + lane] = most[tf];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int tf = 0; tf < 4; ++tf) most[tf] = max(most[tf], mosts[(wn ^ 1) * kTileRows + first + tf * 16 + r]);
+            store_codes(a, col0, row0 + first, rows - first, acc, most, wn == 0);
+        } else {
+            store_values<OUT>(a, col0, row0 + first, rows - first, acc);
+        }
+    }
+}
+
 // ---- launches -------------------------------------------------------------------------------------------------------
 size_t quant_product_workspace(const moe_quant_shape&) { return 256; }
 
+// Experts with at least this many rows run in tiles, the others are streamed.
+constexpr int kTiledMinRows = 65;
+
 template <int OUT>
 static hipError_t launch_out(const QuantArgs& a, hipStream_t stream) {
-    const int grid = 2 * device_cu_count();
-    if (a.rows <= 16) quant_stream_kernel<1, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, a.rows);
-    else if (a.rows <= 32) quant_stream_kernel<2, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, a.rows);
-    else quant_stream_kernel<4, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, a.rows);
+    const int cus = device_cu_count();
+    const int grid = 2 * cus, stream_max = std::min(a.rows, kTiledMinRows - 1);
+    if (a.rows >= kTiledMinRows) quant_tile_kernel<OUT><<<dim3(cus), dim3(kTileWaves * 64), kTileLdsBytes, stream>>>(a, kTiledMinRows);
+    if (a.offsets == nullptr && a.rows >= kTiledMinRows) return hipGetLastError();
+    if (a.rows <= 16) quant_stream_kernel<1, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, stream_max);
+    else if (a.rows <= 32) quant_stream_kernel<2, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, stream_max);
+    else quant_stream_kernel<4, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, stream_max);
     return hipGetLastError();
+}
+
+hipError_t configure_quant_kernels() {
+    for (const void* f : {reinterpret_cast<const void*>(quant_tile_kernel<kOutF32>), reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16>),
+                          reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3>)}) {
+        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kTileLdsBytes);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 hipError_t launch_quant_product(const QuantArgs& a, void*, hipStream_t stream) {
