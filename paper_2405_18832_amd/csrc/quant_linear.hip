@@ -121,6 +121,15 @@ __device__ __forceinline__ int xcd_position() {
 // A wavefront's NF x TF results of 16 columns x 16 rows: columns n0 + 16 nf + 4 (lane / 16) + i, rows row0 + 16 tf + lane % 16, the first
 // `rows` of which exist.
 template <int NF, int TF>
+__device__ __forceinline__ void activate_values(int act, f32x4 (&acc)[NF][TF]) {
+#pragma unroll
+    for (int nf = 0; nf < NF; ++nf)
+#pragma unroll
+        for (int tf = 0; tf < TF; ++tf)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[nf][tf][i] = quant_activate(acc[nf][tf][i], act);
+}
+template <int NF, int TF>
 __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0, f32x4 (&acc)[NF][TF]) {
     const int g = (threadIdx.x & 63) >> 4;
 #pragma unroll
@@ -135,11 +144,8 @@ __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0,
                 for (int tf = 0; tf < TF; ++tf) acc[nf][tf][i] += b;
             }
         }
-#pragma unroll
-        for (int tf = 0; tf < TF; ++tf)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[nf][tf][i] = quant_activate(acc[nf][tf][i], a.act);
     }
+    activate_values(a.act, acc);
 }
 
 template <int OUT, int NF, int TF>
@@ -216,155 +222,290 @@ __device__ __forceinline__ void store_codes(const QuantArgs& a, int n0, int row0
     }
 }
 
-// ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
-// Unit: up to 16 TFMAX rows of an expert x 16 NF WN columns.  WN wavefronts side by side, KS of them share the contraction and add up in
-// LDS in a fixed order.  The weights come from memory straight into registers, a fragment of 2 KiB as two contiguous KiB, D blocks
-// ahead; token rows come through L2.
-template <int TF, int NF, int D>
-__device__ __forceinline__ void stream_sums(const QuantArgs& a, int row0, int rows, const uint8_t* w, const float* sw, int kb0, int kb1,
-                                            f32x4 (&acc)[NF][TF]) {
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
-    const int KB = quant_blocks(a.K);
-    const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
-    const uint8_t* x[TF];
-    const float* sx[TF];
-#pragma unroll
-    for (int tf = 0; tf < TF; ++tf) {
-        const size_t row = source_row(a, row0 + min(tf * 16 + r, rows - 1));
-        x[tf] = a.a + row * pitch + g * 16;
-        sx[tf] = a.a_scales + row * KB;
-    }
-    w += lane * 16;
-    struct Step {
-        i32x8 w[NF], x[TF];
-        float sx[TF], sw;
-    } ring[D];
-    auto load = [&](Step& s, int kb) {
-#pragma unroll
-        for (int nf = 0; nf < NF; ++nf) {
-            const uint8_t* p = w + (static_cast<size_t>(nf) * KB + kb) * kFragBytes;
-            const i32x4 lo = *reinterpret_cast<const i32x4*>(p), hi = *reinterpret_cast<const i32x4*>(p + 1024);
-            s.w[nf] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-#pragma unroll
-        for (int tf = 0; tf < TF; ++tf) {
-            const uint8_t* p = x[tf] + static_cast<size_t>(kb) * kQuantBlock;
-            const i32x4 lo = *reinterpret_cast<const i32x4*>(p), hi = *reinterpret_cast<const i32x4*>(p + 64);
-            s.x[tf] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            s.sx[tf] = sx[tf][kb];
-        }
-        s.sw = sw[kb];
-    };
-    auto add = [&](const Step& s) {
-        Widened wide[NF];
-#pragma unroll
-        for (int nf = 0; nf < NF; ++nf) wide[nf] = widen(s.w[nf]);
-#pragma unroll
-        for (int tf = 0; tf < TF; ++tf) {
-            const Widened x = widen(s.x[tf]);
-            const float scale = s.sx[tf] * s.sw;
-#pragma unroll
-            for (int nf = 0; nf < NF; ++nf) {
-                const f32x4 p = mfma_block(wide[nf], x);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) acc[nf][tf][i] = fmaf(scale, p[i], acc[nf][tf][i]);
-            }
-        }
-    };
-    if (kb0 >= kb1) return;
-    // loads past the end repeat the last block: no load is conditional, so that the loop waits for the oldest ones only
-#pragma unroll
-    for (int i = 0; i < D; ++i) load(ring[i], min(kb0 + i, kb1 - 1));
-    int kb = kb0;
-    for (; kb + D <= kb1; kb += D) {
-#pragma unroll
-        for (int i = 0; i < D; ++i) {
-            add(ring[i]);
-            load(ring[i], min(kb + i + D, kb1 - 1));
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < D; ++i)
-        if (kb + i < kb1) add(ring[i]);
+// ---- copies into LDS ------------------------------------------------------------------------------------------------
+// 4 bytes per lane into LDS, as copy16_to_lds
+__device__ __forceinline__ void copy4_to_lds(const void* src, uint32_t lds_base) {
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(dst) : "memory");
 }
+// The wavefront's copies up to the newest `left` have landed, and with the barrier everybody's; every LDS read before it is done too.
+template <int LEFT>
+__device__ __forceinline__ void copies_landed() {
+    static_assert(LEFT < 64, "vmcnt has six bits");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory");
+}
+__device__ __forceinline__ i32x8 read_codes(const unsigned char* p, int other) {
+    const i32x4 lo = *reinterpret_cast<const i32x4*>(p), hi = *reinterpret_cast<const i32x4*>(p + other);
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// Rows in LDS: 128 bytes each, the 16-byte pieces of a row permuted by its number, so that an operand read (16 rows x one piece) meets no
+// bank twice: piece c of row r lies at c ^ (r / 2 % 8).  A copy brings 8 rows, each a whole line by eight lanes.
+__device__ __forceinline__ int piece_of_lane(int row) { return ((threadIdx.x & 7) ^ (row >> 1 & 7)) << 4; }
+// Where lane l reads piece l / 16 of row `first` + l % 16 (`first` a multiple of 16), and how far from there piece 4 + l / 16 lies.
+__device__ __forceinline__ int row_operand(int first) {
+    const int lane = threadIdx.x & 63, r = lane & 15;
+    return (first + r) * kQuantBlock + (((lane >> 4) ^ (r >> 1)) << 4);
+}
+__device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 : 64; }
 
-template <int TFMAX, int WN, int NF, int KS, int OUT>
-__global__ __launch_bounds__(64 * WN * KS) void quant_stream_kernel(const QuantArgs a, int min_rows, int max_rows) {
-    constexpr int kThreads = 64 * WN * KS, kCols = 16 * NF * WN;
-    static_assert(OUT != kOutE4m3 || kCols == kQuantBlock, "a unit holds the columns that share a scale");
-    __shared__ int32_t starts[MOE_MAX_E + 1], tmp[kThreads / 64];
-    __shared__ f32x4 parts[KS > 1 ? (KS - 1) * WN * NF * TFMAX * 64 : 1];
-    __shared__ uint32_t mosts[OUT == kOutE4m3 ? WN * TFMAX * 16 : 1];
-    count_tiles<kThreads>(a, 16 * TFMAX, min_rows, max_rows, starts, tmp);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wn = wave % WN, ks = wave / WN;
-    const int KB = quant_blocks(a.K), groups = (a.N + kCols - 1) / kCols;
-    const int units = starts[a.E] * groups;
-    const int kb0 = KB * ks / KS, kb1 = KB * (ks + 1) / KS;
-    for (int u = xcd_position(); u < units; u += gridDim.x) {
-        const int e = __builtin_amdgcn_readfirstlane(expert_of(starts, a.E, u / groups));
-        const int tiles = starts[e + 1] - starts[e], local = u - starts[e] * groups;
-        // the tiles of one column group follow each other: they read the same weights
-        const int group = local / tiles, tile = local % tiles;
-        const Segment seg = segment_of(a, e);
-        const int row0 = __builtin_amdgcn_readfirstlane(seg.row0 + tile * 16 * TFMAX);
-        const int rows = __builtin_amdgcn_readfirstlane(min(16 * TFMAX, seg.rows - tile * 16 * TFMAX));
-        const int n0 = __builtin_amdgcn_readfirstlane(group * kCols + wn * 16 * NF);
-        const uint8_t* w = a.w + static_cast<size_t>(e) * quant_matrix_bytes(a.N, a.K) + static_cast<size_t>(n0 / 16) * KB * kFragBytes;
-        const float* sw = a.w_scales + (static_cast<size_t>(e) * quant_blocks(a.N) + n0 / kQuantBlock) * KB;
-        auto run = [&](auto tf_const) {
-            constexpr int TF = decltype(tf_const)::value;
-            f32x4 acc[NF][TF];
+// ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
+// Unit: up to 64 rows of an expert x 128 columns, by 8 wavefronts of 16 columns each, a block of 128 columns of the contraction per
+// step.  Bound by memory, so what matters is that copies never stop: weights (16 KiB a step), rows and scales go to LDS directly, through
+// a ring of six stages that runs on across units.  A block's units follow each other in one row tile, where nothing needs to be looked up
+// (a load that the compiler sees would make it wait for every copy in flight).
+constexpr int kStreamRows = 64, kStreamWaves = 8, kStreamStages = 6, kStreamCopies = 4;
+constexpr int kStreamX = kQuantBlock * kQuantBlock, kStreamS = kStreamX + kStreamRows * kQuantBlock;
+constexpr int kStreamStage = kStreamS + 4 * 256;            // scales of the rows, of the weights (64 times), bias of the 128 columns
+constexpr int kStreamMost = kStreamStages * kStreamStage, kStreamStarts = kStreamMost + kStreamWaves * kStreamRows * 4;
+constexpr int kStreamLdsBytes = kStreamStarts + (MOE_MAX_E + 1 + kStreamWaves) * 4;
+static_assert(kStreamLdsBytes <= 160 * 1024, "fits a CU");
+
+// OUT = kOutParts: the contraction is cut into `split` parts, whose sums go to a.out as [split][rows][pitch of N] fp32.
+constexpr int kOutParts = 3;
+
+template <int OUT>
+__global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int split) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kStreamMost);         // [8][64]
+    int32_t* starts = reinterpret_cast<int32_t*>(smem + kStreamStarts);
+    count_tiles<kStreamWaves * 64>(a, kStreamRows, 1, max_rows, starts, starts + MOE_MAX_E + 1);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
+    const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
+    const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
+    const int per_tile = groups * split, units = starts[a.E] * per_tile;
+
+    // Every block gets the same number of units, as few as the grid allows: a CU can pull more than its share of the memory's rate, so
+    // that a quarter of them idle costs nothing, but a last round of a few units does.  The runs are dealt to the XCDs evenly.
+    const int G = gridDim.x, rounds = (units + G - 1) / G, runs = rounds > 0 ? (units + rounds - 1) / rounds : 0;
+    const int per_xcd = (runs + 7) >> 3, b = blockIdx.x;
+    const int run = G % 8 == 0 ? (b >> 3 < per_xcd ? (b & 7) * per_xcd + (b >> 3) : runs) : b;
+    const int first = run * rounds, last = min(units, first + rounds);
+    if (first >= last) return;
+
+    struct Unit {
+        int u, e, row0, rows, group, kb, kb1, part;
+    };
+    auto unit_at = [&](int u) __attribute__((always_inline)) {
+        Unit w;
+        w.u = u;
+        const int t = u / per_tile, rest = u - t * per_tile;
+        w.e = __builtin_amdgcn_readfirstlane(expert_of(starts, a.E, t));
+        const Segment seg = segment_of(a, w.e);
+        const int tile = __builtin_amdgcn_readfirstlane(t - starts[w.e]);
+        w.row0 = __builtin_amdgcn_readfirstlane(seg.row0 + tile * kStreamRows);
+        w.rows = __builtin_amdgcn_readfirstlane(min(kStreamRows, seg.rows - tile * kStreamRows));
+        w.group = rest / split;
+        w.part = rest - w.group * split;
+        w.kb = KB * w.part / split;
+        w.kb1 = KB * (w.part + 1) / split;
+        return w;
+    };
+    // the next unit of the run, in the same row tile: nothing is looked up
+    auto along = [&](Unit w) __attribute__((always_inline)) {
+        const int part = w.part + 1, over = part == split ? 1 : 0;
+        w.part = over ? 0 : part;
+        w.group += over;
+        w.u += 1;
+        w.kb = KB * w.part / split;
+        w.kb1 = KB * (w.part + 1) / split;
+        return w;
+    };
+    auto new_tile_after = [&](int u) { return (u + 1) % per_tile == 0; };
+
+    // copies: wavefront w brings rows 8 w ... 8 w + 7, weight fragment w, and a quarter of the scales and bias (two wavefronts each)
+    const uint32_t lds = lds_address(smem);
+    const uint32_t to_weights = lds + wave * kFragBytes, to_rows = lds + kStreamX + wave * 1024, to_scales = lds + kStreamS + (wave & 3) * 256;
+    const uint8_t *tile_row, *row_from, *weights_from;
+    const float *tile_scale, *scales_from;
+    int scales_step;
+    auto point_at_tile = [&](const Unit& w) __attribute__((always_inline)) {
+        const int in_tile = wave * 8 + (lane >> 3);
+        tile_row = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(in_tile);
+        tile_scale = a.a_scales + static_cast<size_t>(source_row(a, w.row0 + min(lane, w.rows - 1))) * KB;
+    };
+    auto point_at = [&](const Unit& w) __attribute__((always_inline)) {
+        row_from = tile_row + static_cast<size_t>(w.kb) * kQuantBlock;
+        weights_from = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) +
+                       (static_cast<size_t>(w.group * 8 + wave) * KB + w.kb) * kFragBytes + lane * 16;
+        const int quarter = wave & 3;
+        scales_step = 1;
+        if (quarter == 0) scales_from = tile_scale + w.kb;
+        else if (quarter == 1 || a.bias == nullptr) scales_from = a.w_scales + (static_cast<size_t>(w.e) * groups + w.group) * KB + w.kb;
+        else {
+            scales_from = a.bias + static_cast<size_t>(w.e) * a.N + min(w.group * kQuantBlock + (quarter - 2) * 64 + lane, a.N - 1);
+            scales_step = 0;
+        }
+    };
+    auto stage_in = [&](int slot) {
+        const int at = slot * kStreamStage;
+        copy16_to_lds(weights_from, to_weights + at);
+        copy16_to_lds(weights_from + 1024, to_weights + at + 1024);
+        copy16_to_lds(row_from, to_rows + at);
+        copy4_to_lds(scales_from, to_scales + at);
+        weights_from += kFragBytes;
+        row_from += kQuantBlock;
+        scales_from += scales_step;
+    };
+
+    Unit ahead = unit_at(first);            // the unit that is being copied
+    point_at_tile(ahead);
+    point_at(ahead);
+    int slot_in = 0;
+    bool copying = true;
+    auto copy_next = [&]() __attribute__((always_inline)) {
+        if (copying) {
+            stage_in(slot_in);
+        } else {
+            // nothing left to copy: copies of some scale to the slot that has fallen free keep up the count that the waits go by
 #pragma unroll
-            for (int nf = 0; nf < NF; ++nf)
-#pragma unroll
-                for (int tf = 0; tf < TF; ++tf) acc[nf][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
-            stream_sums<TF, NF, (TF <= 2 ? 4 : 3)>(a, row0, rows, w, sw, kb0, kb1, acc);
-            if constexpr (KS > 1) {
-                f32x4* part = parts + (wn * NF * TF) * 64 + lane;
-                if (ks > 0) {
-#pragma unroll
-                    for (int nf = 0; nf < NF; ++nf)
-#pragma unroll
-                        for (int tf = 0; tf < TF; ++tf) part[((ks - 1) * WN * NF * TF + nf * TF + tf) * 64] = acc[nf][tf];
+            for (int i = 0; i < kStreamCopies; ++i) copy4_to_lds(tile_scale, to_scales + slot_in * kStreamStage);
+        }
+        slot_in = slot_in == kStreamStages - 1 ? 0 : slot_in + 1;
+        ++ahead.kb;
+        if (ahead.kb == ahead.kb1) {
+            if (ahead.u + 1 < last) {
+                if (new_tile_after(ahead.u)) {
+                    ahead = unit_at(ahead.u + 1);
+                    point_at_tile(ahead);
+                } else {
+                    ahead = along(ahead);
                 }
-                __syncthreads();
-                if (ks == 0) {
-#pragma unroll
-                    for (int s = 1; s < KS; ++s)
-#pragma unroll
-                        for (int nf = 0; nf < NF; ++nf)
-#pragma unroll
-                            for (int tf = 0; tf < TF; ++tf) acc[nf][tf] += part[((s - 1) * WN * NF * TF + nf * TF + tf) * 64];
-                }
+                point_at(ahead);
+            } else {
+                copying = false;
             }
-            if (ks == 0) finish_values(a, e, n0, acc);
-            if constexpr (OUT == kOutE4m3) {
-                uint32_t most[TF];
-                if (ks == 0) {
+        }
+    };
+#pragma unroll 1
+    for (int i = 0; i < kStreamStages - 1; ++i) copy_next();
+
+    Unit cur = unit_at(first);
+    const int at_w = wave * kFragBytes + lane * 16, at_x = kStreamX + row_operand(0), x_other = row_operand_other(at_x);
+    const int at_sx = kStreamS + r * 4, at_sw = kStreamS + 256, at_bias = kStreamS + 512 + (wave * 16 + (lane >> 4) * 4) * 4;
+    int slot = 0;
+    while (true) {
+        auto run_unit = [&](auto tf_const) __attribute__((always_inline)) {
+            constexpr int TF = decltype(tf_const)::value;
+            f32x4 acc[1][TF];
+#pragma unroll
+            for (int tf = 0; tf < TF; ++tf) acc[0][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
+            f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+            for (; cur.kb < cur.kb1; ++cur.kb) {
+                copies_landed<(kStreamStages - 2) * kStreamCopies>();
+                copy_next();
+                const unsigned char* st = smem + slot * kStreamStage;
+                const float sw = *reinterpret_cast<const float*>(st + at_sw);
+                const Widened w = widen(read_codes(st + at_w, 1024));
+                i32x8 x[TF];
+                float sx[TF];
+#pragma unroll
+                for (int tf = 0; tf < TF; ++tf) {
+                    x[tf] = read_codes(st + at_x + tf * kFragBytes, x_other);
+                    sx[tf] = *reinterpret_cast<const float*>(st + at_sx + tf * 64);
+                }
+                if (cur.kb + 1 == cur.kb1) bias = *reinterpret_cast<const f32x4*>(st + at_bias);
+#pragma unroll
+                for (int tf = 0; tf < TF; ++tf) {
+                    const f32x4 p = mfma_block(w, widen(x[tf]));
+                    const float scale = sx[tf] * sw;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[0][tf][i] = fmaf(scale, p[i], acc[0][tf][i]);
+                }
+                slot = slot == kStreamStages - 1 ? 0 : slot + 1;
+            }
+            const int n0 = cur.group * kQuantBlock + wave * 16;
+            if constexpr (OUT == kOutParts) {
+                float* parts = static_cast<float*>(a.out) + static_cast<size_t>(cur.part) * a.rows * quant_pitch(a.N);
+#pragma unroll
+                for (int tf = 0; tf < TF; ++tf)
+                    if (tf * 16 + r < cur.rows)
+                        *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(cur.row0 + tf * 16 + r) * quant_pitch(a.N) + n0 + (lane >> 4) * 4) =
+                            acc[0][tf];
+            } else {
+                if (a.bias != nullptr) {
+#pragma unroll
+                    for (int tf = 0; tf < TF; ++tf) acc[0][tf] += bias;
+                }
+                activate_values(a.act, acc);
+                if constexpr (OUT == kOutE4m3) {
+                    uint32_t most[TF];
                     row_magnitudes(a.N, n0, acc, most);
                     if (lane < 16) {
 #pragma unroll
-                        for (int tf = 0; tf < TF; ++tf) mosts[wn * TFMAX * 16 + tf * 16 + lane] = most[tf];
+                        for (int tf = 0; tf < TF; ++tf) mosts[wave * kStreamRows + tf * 16 + lane] = most[tf];
                     }
-                }
-                __syncthreads();
-                if (ks == 0) {
+                    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
                     for (int tf = 0; tf < TF; ++tf)
 #pragma unroll
-                        for (int v = 0; v < WN; ++v) most[tf] = max(most[tf], mosts[v * TFMAX * 16 + tf * 16 + (lane & 15)]);
-                    store_codes(a, n0, row0, rows, acc, most, wn == 0);
+                        for (int v = 0; v < kStreamWaves; ++v) most[tf] = max(most[tf], mosts[v * kStreamRows + tf * 16 + r]);
+                    store_codes(a, n0, cur.row0, cur.rows, acc, most, wave == 0);
+                } else {
+                    store_values<OUT>(a, n0, cur.row0, cur.rows, acc);
                 }
-            } else {
-                if (ks == 0) store_values<OUT>(a, n0, row0, rows, acc);
             }
         };
-        const int tf = (rows + 15) >> 4;
-        if (TFMAX == 1 || tf == 1) run(std::integral_constant<int, 1>{});
-        else if (TFMAX == 2 || tf == 2) run(std::integral_constant<int, (TFMAX < 2 ? TFMAX : 2)>{});
-        else run(std::integral_constant<int, TFMAX>{});
-        if constexpr (KS > 1 || OUT == kOutE4m3) __syncthreads();       // the LDS is the next unit's
+        const int tf = (cur.rows + 15) >> 4;
+        if (tf == 1) run_unit(std::integral_constant<int, 1>{});
+        else if (tf == 2) run_unit(std::integral_constant<int, 2>{});
+        else run_unit(std::integral_constant<int, 4>{});
+        if (cur.u + 1 >= last) break;
+        cur = new_tile_after(cur.u) ? unit_at(cur.u + 1) : along(cur);
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
+}
+
+// Adds up the parts of a split contraction, in their order, and finishes the rows.  A block of threads per row and 8 groups of 128
+// columns; four columns per thread.
+template <int OUT>
+__global__ __launch_bounds__(256) void quant_join_kernel(const QuantArgs a, const float* __restrict__ parts, int split) {
+    const int row = blockIdx.x, lane = threadIdx.x & 63;
+    __shared__ int32_t before;
+    int e = 0;
+    if (a.offsets != nullptr) {            // the expert whose rows this one is among
+        if (threadIdx.x == 0) before = 0;
+        __syncthreads();
+        int n = 0;
+        for (int i = threadIdx.x; i < a.E; i += 256) n += a.offsets[i + 1] <= row ? 1 : 0;
+        atomicAdd(&before, n);
+        __syncthreads();
+        e = before;
+        if (e >= a.E) return;
+        const Segment seg = segment_of(a, e);
+        if (row < seg.row0 || row >= seg.row0 + seg.rows) return;
+    }
+    const int n0 = (blockIdx.y * 256 + threadIdx.x) * 4;
+    const size_t pitch = quant_pitch(a.N);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (n0 < static_cast<int>(pitch)) {
+        const float* p = parts + static_cast<size_t>(row) * pitch + n0;
+        for (int s = 0; s < split; ++s) v += *reinterpret_cast<const f32x4*>(p + static_cast<size_t>(s) * a.rows * pitch);
+    }
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (n0 + i >= a.N) v[i] = 0.f;
+        else v[i] = quant_activate(a.bias != nullptr ? v[i] + a.bias[static_cast<size_t>(e) * a.N + n0 + i] : v[i], a.act);
+        most = max(most, magnitude(v[i]));
+    }
+    if constexpr (OUT == kOutE4m3) {
+        most = row16_max(most);
+        most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16, 64)));       // 32 lanes are a block of 128
+        const float scale = block_scale(most), inv = 1.f / scale;
+        if (n0 < static_cast<int>(pitch)) {
+            uint32_t codes = pack_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            if (n0 + 4 > a.N) codes = n0 >= a.N ? 0u : codes & (0xffffffffu >> (8 * (n0 + 4 - a.N)));
+            *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.out) + row * pitch + n0) = codes;
+            if ((lane & 31) == 0) a.out_scales[static_cast<size_t>(row) * quant_blocks(a.N) + n0 / kQuantBlock] = scale;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n0 + i < a.N) {
+                const size_t at = static_cast<size_t>(row) * a.N + n0 + i;
+                if constexpr (OUT == kOutF32) static_cast<float*>(a.out)[at] = v[i];
+                else static_cast<uint16_t*>(a.out)[at] = f32_to_bf16(v[i]);
+            }
     }
 }
 
@@ -372,8 +513,7 @@ __global__ __launch_bounds__(64 * WN * KS) void quant_stream_kernel(const QuantA
 // Unit: 256 rows x 128 columns by 8 wavefronts (4 x 2, 64 x 64 each), a block of 128 columns of the contraction per step, through a
 // ring of three LDS stages: one being read, one that has landed (its first fragments are read ahead), one in flight.  Everything goes from
 // memory to LDS directly, 16 bytes per lane; a stage holds
-//   rows     [256][128 bytes], copied a whole line per eight lanes; the 16-byte pieces of a row are permuted by its number so that the
-//            operand reads (16 rows x one piece) meet no bank twice: piece c of row r lies at c ^ (r / 2 % 8)
+//   rows     [256][128 bytes]
 //   weights  8 fragments of 2 KiB as they are packed, 16 rows each
 //   scales   of the 256 rows, and the weights' (one for the unit's 128 columns)
 constexpr int kTileRows = 256, kTileCols = kQuantBlock, kTileWaves = 8, kTileStages = 3;
@@ -381,12 +521,6 @@ constexpr int kStageW = kTileRows * kQuantBlock, kStageS = kStageW + kTileCols *
 constexpr int kTileMost = kTileStages * kStage, kTileStarts = kTileMost + 2 * kTileRows * 4;
 constexpr int kTileLdsBytes = kTileStarts + (MOE_MAX_E + 1 + kTileWaves) * 4;
 static_assert(kTileLdsBytes <= 160 * 1024, "fits a CU");
-
-// 4 bytes per lane into LDS, as copy16_to_lds
-__device__ __forceinline__ void copy4_to_lds(const void* src, uint32_t lds_base) {
-    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
-    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(dst) : "memory");
-}
 
 template <int OUT>
 __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const QuantArgs a, int min_rows) {
@@ -403,8 +537,7 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
     // copies: wavefront w brings rows 32 w ... 32 w + 31, weight fragment w, and the scales of rows 64 (w % 4) ... or of the weights
     const uint32_t to_rows = lds + wave * 4096, to_weights = lds + kStageW + wave * 2048;
     const uint32_t to_scales = lds + kStageS + (wave < 4 ? wave * 256 : kTileRows * 4);
-    // operand reads: piece g of row r, the other half's piece 4 + g is 64 bytes away by exclusive or
-    const int at_x = (wm * 64 + r) * kQuantBlock + ((g ^ (r >> 1)) << 4), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
+    const int at_x = row_operand(wm * 64), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
     const int at_sx = kStageS + (wm * 64 + r) * 4, at_sw = kStageS + kTileRows * 4;
 
     for (int u = xcd_position(); u < units; u += gridDim.x) {
@@ -426,7 +559,7 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         for (int i = 0; i < 4; ++i) {
             const int in_tile = wave * 32 + i * 8 + (lane >> 3);
             const size_t row = source_row(a, row0 + min(in_tile, rows - 1));
-            from_rows[i] = a.a + row * pitch + (((lane & 7) ^ (in_tile >> 1 & 7)) << 4);
+            from_rows[i] = a.a + row * pitch + piece_of_lane(in_tile);
         }
         if (wave < 4) from_scales = a.a_scales + static_cast<size_t>(source_row(a, row0 + min(wave * 64 + lane, rows - 1))) * KB;
         else from_scales = a.w_scales + (static_cast<size_t>(e) * groups + group) * KB;
@@ -449,16 +582,11 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
 #pragma unroll
             for (int tf = 0; tf < 4; ++tf) acc[nf][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");       // the ring is free
+        copies_landed<0>();         // the ring is free
         stage_in(0);
         if (KB > 1) stage_in(1);
-        if (KB > 1) asm volatile("s_waitcnt vmcnt(7)\n\ts_barrier" ::: "memory");
-        else asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        auto read_codes = [&](const unsigned char* p, int other) {
-            const i32x4 lo = *reinterpret_cast<const i32x4*>(p), hi = *reinterpret_cast<const i32x4*>(p + other);
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        const int x_other = (at_x & 64) ? -64 : 64;
+        if (KB > 1) copies_landed<7>();
+        else copies_landed<0>();
         Widened w[4];
 #pragma unroll
         for (int nf = 0; nf < 4; ++nf) w[nf] = widen(read_codes(smem + at_w + nf * kFragBytes, 1024));
@@ -469,7 +597,7 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
             const unsigned char* st = smem + slot * kStage;
             const unsigned char* st_next = smem + next * kStage;
             const bool more = j + 1 < KB;
-            if (more) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            if (more) copies_landed<0>();
             if (j + 2 < KB) stage_in(after);
             const float sw = *reinterpret_cast<const float*>(st + at_sw);
 #pragma unroll
@@ -508,36 +636,63 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
-size_t quant_product_workspace(const moe_quant_shape&) { return 256; }
-
 // Experts with at least this many rows run in tiles, the others are streamed.
 constexpr int kTiledMinRows = 65;
 
+// Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave most CUs without one.
+// A grouped call's number of row tiles is not known here; half of the most it can be is taken.
+static int stream_split(int rows, int N, int K, int E) {
+    if (rows >= kTiledMinRows) return 1;
+    const int tiles = E == 1 ? 1 : (std::min(rows, E) + 1) / 2;
+    const int units = tiles * quant_blocks(N);
+    return std::max(1, std::min(256 / units, quant_blocks(K) / 2));
+}
+
+size_t quant_product_workspace(const moe_quant_shape& s) {
+    const int split = stream_split(s.rows, s.N, s.K, s.E);
+    const size_t parts = split > 1 ? static_cast<size_t>(split) * s.rows * quant_pitch(s.N) * sizeof(float) : 0;
+    return (std::max<size_t>(parts, 1) + 255) / 256 * 256;
+}
+
 template <int OUT>
-static hipError_t launch_out(const QuantArgs& a, hipStream_t stream) {
-    const int cus = device_cu_count();
-    const int grid = 2 * cus, stream_max = std::min(a.rows, kTiledMinRows - 1);
-    if (a.rows >= kTiledMinRows) quant_tile_kernel<OUT><<<dim3(cus), dim3(kTileWaves * 64), kTileLdsBytes, stream>>>(a, kTiledMinRows);
-    if (a.offsets == nullptr && a.rows >= kTiledMinRows) return hipGetLastError();
-    if (a.rows <= 16) quant_stream_kernel<1, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, stream_max);
-    else if (a.rows <= 32) quant_stream_kernel<2, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, stream_max);
-    else quant_stream_kernel<4, 4, 2, 2, OUT><<<dim3(grid), dim3(512), 0, stream>>>(a, 1, stream_max);
+static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
+    const dim3 grid(device_cu_count()), threads(kStreamWaves * 64);
+    const int split = stream_split(a.rows, a.N, a.K, a.E);
+    if (split > 1) {
+        QuantArgs parts = a;
+        parts.out = ws;
+        quant_stream_kernel<kOutParts><<<grid, threads, kStreamLdsBytes, stream>>>(parts, a.rows, split);
+        quant_join_kernel<OUT><<<dim3(a.rows, (quant_blocks(a.N) + 7) / 8), dim3(256), 0, stream>>>(a, static_cast<const float*>(ws), split);
+        return hipGetLastError();
+    }
+    if (a.rows >= kTiledMinRows) quant_tile_kernel<OUT><<<grid, dim3(kTileWaves * 64), kTileLdsBytes, stream>>>(a, kTiledMinRows);
+    if (a.offsets != nullptr || a.rows < kTiledMinRows)
+        quant_stream_kernel<OUT><<<grid, threads, kStreamLdsBytes, stream>>>(a, std::min(a.rows, kTiledMinRows - 1), 1);
     return hipGetLastError();
 }
 
 hipError_t configure_quant_kernels() {
-    for (const void* f : {reinterpret_cast<const void*>(quant_tile_kernel<kOutF32>), reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16>),
-                          reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3>)}) {
-        const hipError_t e = hipFuncSetAttribute(f, hipFuncAttributeMaxDynamicSharedMemorySize, kTileLdsBytes);
+    const struct {
+        const void* kernel;
+        int lds;
+    } all[] = {{reinterpret_cast<const void*>(quant_tile_kernel<kOutF32>), kTileLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16>), kTileLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3>), kTileLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutF32>), kStreamLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutBf16>), kStreamLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutE4m3>), kStreamLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutParts>), kStreamLdsBytes}};
+    for (const auto& k : all) {
+        const hipError_t e = hipFuncSetAttribute(k.kernel, hipFuncAttributeMaxDynamicSharedMemorySize, k.lds);
         if (e != hipSuccess) return e;
     }
     return hipSuccess;
 }
 
-hipError_t launch_quant_product(const QuantArgs& a, void*, hipStream_t stream) {
-    if (a.out_dtype == MOE_F32) return launch_out<kOutF32>(a, stream);
-    if (a.out_dtype == MOE_BF16) return launch_out<kOutBf16>(a, stream);
-    return launch_out<kOutE4m3>(a, stream);
+hipError_t launch_quant_product(const QuantArgs& a, void* ws, hipStream_t stream) {
+    if (a.out_dtype == MOE_F32) return launch_out<kOutF32>(a, ws, stream);
+    if (a.out_dtype == MOE_BF16) return launch_out<kOutBf16>(a, ws, stream);
+    return launch_out<kOutE4m3>(a, ws, stream);
 }
 
 }  // namespace moe
