@@ -208,7 +208,7 @@ __device__ __forceinline__ void store_codes(const QuantArgs& a, int n0, int row0
     for (int tf = 0; tf < TF; ++tf) {
         if (tf * 16 + r >= rows) continue;
         const size_t row = static_cast<size_t>(row0 + tf * 16 + r);
-        const float scale = block_scale(most[tf]), inv = 1.f / scale;
+        const float scale = block_scale(most[tf]), inv = __builtin_amdgcn_rcpf(scale);
         uint8_t* out = static_cast<uint8_t*>(a.out) + row * pitch;
 #pragma unroll
         for (int nf = 0; nf < NF; ++nf) {
@@ -264,9 +264,10 @@ static_assert(kStreamLdsBytes <= 160 * 1024, "fits a CU");
 constexpr int kOutParts = 3;
 
 template <int OUT>
-__global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int split) {
+__global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
+    const int split = OUT == kOutParts ? parts_wanted : 1;
     extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kStreamMost);         // [8][64]
+    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kStreamMost);         // [64][8]
     int32_t* starts = reinterpret_cast<int32_t*>(smem + kStreamStarts);
     count_tiles<kStreamWaves * 64>(a, kStreamRows, 1, max_rows, starts, starts + MOE_MAX_E + 1);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
@@ -283,12 +284,12 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
     if (first >= last) return;
 
     struct Unit {
-        int u, e, row0, rows, group, kb, kb1, part;
+        int tile, rest, e, row0, rows, group, kb, kb1, part;    // number `rest` of row tile `tile`
     };
-    auto unit_at = [&](int u) __attribute__((always_inline)) {
+    auto unit_at = [&](int t, int rest) __attribute__((always_inline)) {
         Unit w;
-        w.u = u;
-        const int t = u / per_tile, rest = u - t * per_tile;
+        w.tile = t;
+        w.rest = rest;
         w.e = __builtin_amdgcn_readfirstlane(expert_of(starts, a.E, t));
         const Segment seg = segment_of(a, w.e);
         const int tile = __builtin_amdgcn_readfirstlane(t - starts[w.e]);
@@ -305,12 +306,11 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
         const int part = w.part + 1, over = part == split ? 1 : 0;
         w.part = over ? 0 : part;
         w.group += over;
-        w.u += 1;
+        w.rest += 1;
         w.kb = KB * w.part / split;
         w.kb1 = KB * (w.part + 1) / split;
         return w;
     };
-    auto new_tile_after = [&](int u) { return (u + 1) % per_tile == 0; };
 
     // copies: wavefront w brings rows 8 w ... 8 w + 7, weight fragment w, and a quarter of the scales and bias (two wavefronts each)
     const uint32_t lds = lds_address(smem);
@@ -347,7 +347,9 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
         scales_from += scales_step;
     };
 
-    Unit ahead = unit_at(first);            // the unit that is being copied
+    const int tile0 = first / per_tile;
+    Unit ahead = unit_at(tile0, first - tile0 * per_tile);      // the unit that is being copied
+    int units_in = last - first, units_out = units_in;
     point_at_tile(ahead);
     point_at(ahead);
     int slot_in = 0;
@@ -363,9 +365,9 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
         slot_in = slot_in == kStreamStages - 1 ? 0 : slot_in + 1;
         ++ahead.kb;
         if (ahead.kb == ahead.kb1) {
-            if (ahead.u + 1 < last) {
-                if (new_tile_after(ahead.u)) {
-                    ahead = unit_at(ahead.u + 1);
+            if (--units_in > 0) {
+                if (ahead.rest + 1 == per_tile) {
+                    ahead = unit_at(ahead.tile + 1, 0);
                     point_at_tile(ahead);
                 } else {
                     ahead = along(ahead);
@@ -379,7 +381,7 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
 #pragma unroll 1
     for (int i = 0; i < kStreamStages - 1; ++i) copy_next();
 
-    Unit cur = unit_at(first);
+    Unit cur = unit_at(tile0, first - tile0 * per_tile);
     const int at_w = wave * kFragBytes + lane * 16, at_x = kStreamX + row_operand(0), x_other = row_operand_other(at_x);
     const int at_sx = kStreamS + r * 4, at_sw = kStreamS + 256, at_bias = kStreamS + 512 + (wave * 16 + (lane >> 4) * 4) * 4;
     int slot = 0;
@@ -432,13 +434,16 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
                     row_magnitudes(a.N, n0, acc, most);
                     if (lane < 16) {
 #pragma unroll
-                        for (int tf = 0; tf < TF; ++tf) mosts[wave * kStreamRows + tf * 16 + lane] = most[tf];
+                        for (int tf = 0; tf < TF; ++tf) mosts[(tf * 16 + lane) * kStreamWaves + wave] = most[tf];
                     }
                     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
                     for (int tf = 0; tf < TF; ++tf)
 #pragma unroll
-                        for (int v = 0; v < kStreamWaves; ++v) most[tf] = max(most[tf], mosts[v * kStreamRows + tf * 16 + r]);
+                        for (int v = 0; v < kStreamWaves; v += 4) {
+                            const uint4 m = *reinterpret_cast<const uint4*>(mosts + (tf * 16 + r) * kStreamWaves + v);
+                            most[tf] = max(most[tf], max(max(m.x, m.y), max(m.z, m.w)));
+                        }
                     store_codes(a, n0, cur.row0, cur.rows, acc, most, wave == 0);
                 } else {
                     store_values<OUT>(a, n0, cur.row0, cur.rows, acc);
@@ -449,8 +454,8 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
         if (tf == 1) run_unit(std::integral_constant<int, 1>{});
         else if (tf == 2) run_unit(std::integral_constant<int, 2>{});
         else run_unit(std::integral_constant<int, 4>{});
-        if (cur.u + 1 >= last) break;
-        cur = new_tile_after(cur.u) ? unit_at(cur.u + 1) : along(cur);
+        if (--units_out == 0) break;
+        cur = cur.rest + 1 == per_tile ? unit_at(cur.tile + 1, 0) : along(cur);
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
 }
