@@ -18,22 +18,27 @@ enum OutKind { kOutF32 = 0, kOutBf16 = 1, kOutE4m3 = 2 };
 struct Widened {
     bf16x8 v[4];
 };
+__device__ __forceinline__ bf16x8 widen8(int32_t lo, int32_t hi) {
+    union {
+        bf16x2_t two[4];
+        bf16x8 eight;
+    } u;
+    u.two[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+    u.two[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    u.two[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+    u.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    return u.eight;
+}
 __device__ __forceinline__ Widened widen(const i32x8& codes) {
     Widened r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        union {
-            bf16x2_t two[4];
-            bf16x8 eight;
-        } u;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            u.two[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i + j], 1.f, false);
-            u.two[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes[2 * i + j], 1.f, true);
-        }
-        r.v[i] = u.eight;
-    }
+    for (int i = 0; i < 4; ++i) r.v[i] = widen8(codes[2 * i], codes[2 * i + 1]);
     return r;
+}
+// Half of them: the values of codes 16 half ... 16 half + 15.
+__device__ __forceinline__ void widen_half(const i32x8& codes, int half, Widened& r) {
+#pragma unroll
+    for (int i = 2 * half; i < 2 * half + 2; ++i) r.v[i] = widen8(codes[2 * i], codes[2 * i + 1]);
 }
 
 // 16 x 16 results of one block of 128 columns: first operand 16 weight rows, second 16 token rows.  Lane l holds 32 codes of row
@@ -65,41 +70,67 @@ __device__ __forceinline__ Segment segment_of(const QuantArgs& a, int e) {
     const int lo = min(max(a.offsets[e], 0), a.rows), hi = min(max(a.offsets[e + 1], lo), a.rows);
     return Segment{lo, hi - lo};
 }
+// The same for an expert that runs, its number the same for the whole wavefront, by scalar loads: they are not counted with the copies into LDS.
+__device__ __forceinline__ Segment segment_of_unit(const QuantArgs& a, int e) {
+    if (a.offsets == nullptr) return Segment{0, a.rows};
+    const auto* offsets = (const __attribute__((address_space(4))) int32_t*)a.offsets;
+    const int lo = min(max(offsets[e], 0), a.rows), hi = min(max(offsets[e + 1], lo), a.rows);
+    return Segment{lo, hi - lo};
+}
 // Row of `a` that row p of the product reads.
 __device__ __forceinline__ int source_row(const QuantArgs& a, int p) {
     if (a.perm == nullptr) return p;
     return min(max(a.perm[p], 0), a.rows - 1) / a.k;
 }
 
-// Row tiles before each expert, starts[0 ... E], counted by every block for itself: E is at most 1024, a list in memory would cost
-// a launch.  Experts outside [min_rows, max_rows] have none.  `tmp`: 17 ints.
+// Row tiles of the experts of at least min_rows rows, counted by every block for itself: E is at most 1024, a list in memory would cost
+// a launch.  whole[e] is the number of tiles of `tile_rows` rows that the experts before e have, whole[E] that of all; `rest` lists the
+// experts with a shorter last tile, those of more than 128 rows first, then of more than 64, then the others, so that units of one length
+// are handed out together.  Returns how many of these there are.  `tmp`: four ints per wavefront.
 template <int THREADS>
-__device__ __forceinline__ void count_tiles(const QuantArgs& a, int tile_rows, int min_rows, int max_rows, int32_t* starts, int32_t* tmp) {
+__device__ __forceinline__ int count_tiles(const QuantArgs& a, int tile_rows, int min_rows, int32_t* whole, uint16_t* rest, int4* tmp) {
     constexpr int W = THREADS / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int before = 0;
-    for (int e0 = 0; e0 < a.E; e0 += THREADS) {
-        const int e = e0 + threadIdx.x;
-        int n = 0;
-        if (e < a.E) {
-            const int m = segment_of(a, e).rows;
-            if (m >= min_rows && m <= max_rows) n = (m + tile_rows - 1) / tile_rows;
+    int4 before = {0, 0, 0, 0};            // whole tiles, and last tiles by length
+    int kind_base[3] = {0, 0, 0};
+    // the lengths' totals are needed before the first expert's place is known: first pass counts, second one places
+    for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 1) {
+            kind_base[1] = before.y;
+            kind_base[2] = before.y + before.z;
+            if (threadIdx.x == 0) whole[a.E] = before.x;
+            before = int4{0, 0, 0, 0};
         }
-        const int incl = wave_scan(n);
-        if (lane == 63) tmp[wave] = incl;
-        __syncthreads();
-        int mine = before;
-        for (int w = 0; w < W; ++w) {
-            if (w < wave) mine += tmp[w];
-            before += tmp[w];
+        for (int e0 = 0; e0 < a.E; e0 += THREADS) {
+            const int e = e0 + threadIdx.x;
+            int m = e < a.E ? segment_of(a, e).rows : 0;
+            if (m < min_rows) m = 0;
+            const int n = m / tile_rows, left = m - n * tile_rows;
+            const int kind = left == 0 ? -1 : left > 128 ? 0 : left > 64 ? 1 : 2;
+            const int incl = wave_scan(n);
+            const uint64_t k0 = __ballot(kind == 0), k1 = __ballot(kind == 1), k2 = __ballot(kind == 2);
+            if (lane == 63) tmp[wave] = int4{incl, __popcll(k0), __popcll(k1), __popcll(k2)};
+            __syncthreads();
+            int4 mine = before;
+            for (int w = 0; w < W; ++w) {
+                const int4 t = tmp[w];
+                if (w < wave) mine = int4{mine.x + t.x, mine.y + t.y, mine.z + t.z, mine.w + t.w};
+                before = int4{before.x + t.x, before.y + t.y, before.z + t.z, before.w + t.w};
+            }
+            if (pass == 1) {
+                if (e < a.E) whole[e] = mine.x + incl - n;
+                const uint64_t below = (1ull << lane) - 1;
+                const int at = kind == 0 ? mine.y + __popcll(k0 & below)
+                             : kind == 1 ? kind_base[1] + mine.z + __popcll(k1 & below)
+                                         : kind_base[2] + mine.w + __popcll(k2 & below);
+                if (kind >= 0) rest[at] = static_cast<uint16_t>(e);
+            }
+            __syncthreads();
         }
-        if (e < a.E) starts[e] = mine + incl - n;
-        __syncthreads();
     }
-    if (threadIdx.x == 0) starts[a.E] = before;
-    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(before.y + before.z + before.w);
 }
-// The expert that tile t belongs to: the last whose tiles begin at or before t.  By whole wavefronts.
+// The expert that tile t of a list belongs to: the last whose tiles begin at or before t.  By whole wavefronts.
 __device__ __forceinline__ int expert_of(const int32_t* starts, int E, int t) {
     if (E == 1) return 0;
     const int lane = threadIdx.x & 63;
@@ -118,16 +149,26 @@ __device__ __forceinline__ int xcd_position() {
 }
 
 // ---- what becomes of a tile's sums ----------------------------------------------------------------------------------
-// A wavefront's NF x TF results of 16 columns x 16 rows: columns n0 + 16 nf + 4 (lane / 16) + i, rows row0 + 16 tf + lane % 16, the first
-// `rows` of which exist.
+// A wavefront's NF x TF results of 16 columns x 16 rows: columns n0 + 16 nf + 4 (lane / 16) + i, rows row0 + STRIDE tf + lane % 16; of the
+// rows from row0 on, `rows` exist.
 template <int NF, int TF>
 __device__ __forceinline__ void activate_values(int act, f32x4 (&acc)[NF][TF]) {
+    if (act == MOE_ACT_GELU) {
 #pragma unroll
-    for (int nf = 0; nf < NF; ++nf)
+        for (int nf = 0; nf < NF; ++nf)
 #pragma unroll
-        for (int tf = 0; tf < TF; ++tf)
+            for (int tf = 0; tf < TF; ++tf) {
+                acc[nf][tf] = activate4<MOE_ACT_GELU>(acc[nf][tf]);
+                if (NF * TF > 4) __builtin_amdgcn_sched_barrier(0);        // many values at once would need registers that there are not
+            }
+    } else if (act == MOE_ACT_RELU) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) acc[nf][tf][i] = quant_activate(acc[nf][tf][i], act);
+        for (int nf = 0; nf < NF; ++nf)
+#pragma unroll
+            for (int tf = 0; tf < TF; ++tf)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[nf][tf][i] = acc[nf][tf][i] < 0.f ? 0.f : acc[nf][tf][i];        // NaN stays
+    }
 }
 template <int NF, int TF>
 __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0, f32x4 (&acc)[NF][TF]) {
@@ -148,7 +189,7 @@ __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0,
     activate_values(a.act, acc);
 }
 
-template <int OUT, int NF, int TF>
+template <int OUT, int STRIDE, int NF, int TF>
 __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row0, int rows, const f32x4 (&acc)[NF][TF]) {
     static_assert(OUT != kOutE4m3, "");
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
@@ -156,8 +197,8 @@ __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row
     const bool wide = a.N % 4 == 0 && reinterpret_cast<uintptr_t>(a.out) % (OUT == kOutF32 ? 16 : 8) == 0;
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
-        if (tf * 16 + r >= rows) continue;
-        const size_t at = static_cast<size_t>(row0 + tf * 16 + r) * a.N;
+        if (tf * STRIDE + r >= rows) continue;
+        const size_t at = static_cast<size_t>(row0 + tf * STRIDE + r) * a.N;
 #pragma unroll
         for (int nf = 0; nf < NF; ++nf) {
             const int n = n0 + nf * 16 + g * 4;
@@ -199,15 +240,15 @@ __device__ __forceinline__ void row_magnitudes(int N, int n0, f32x4 (&acc)[NF][T
 }
 
 // Codes of a block of 128 columns whose rows' largest magnitudes are known; the wavefront with `scales` also stores the scales.
-template <int NF, int TF>
+template <int STRIDE, int NF, int TF>
 __device__ __forceinline__ void store_codes(const QuantArgs& a, int n0, int row0, int rows, const f32x4 (&acc)[NF][TF],
                                             const uint32_t (&most)[TF], bool scales) {
     const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const size_t pitch = quant_pitch(a.N);
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
-        if (tf * 16 + r >= rows) continue;
-        const size_t row = static_cast<size_t>(row0 + tf * 16 + r);
+        if (tf * STRIDE + r >= rows) continue;
+        const size_t row = static_cast<size_t>(row0 + tf * STRIDE + r);
         const float scale = block_scale(most[tf]), inv = __builtin_amdgcn_rcpf(scale);
         uint8_t* out = static_cast<uint8_t*>(a.out) + row * pitch;
 #pragma unroll
@@ -249,16 +290,40 @@ __device__ __forceinline__ int row_operand(int first) {
 __device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 : 64; }
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
-// Unit: up to 64 rows of an expert x 128 columns, by 8 wavefronts of 16 columns each, a block of 128 columns of the contraction per
+// Unit: an expert's rows, at most 64, x 128 columns, by 8 wavefronts of 16 columns each, a block of 128 columns of the contraction per
 // step.  Bound by memory, so what matters is that copies never stop: weights (16 KiB a step), rows and scales go to LDS directly, through
-// a ring of six stages that runs on across units.  A block's units follow each other in one row tile, where nothing needs to be looked up
+// a ring of six stages that runs on across units.  A block's units follow each other in one expert, where nothing needs to be looked up
 // (a load that the compiler sees would make it wait for every copy in flight).
 constexpr int kStreamRows = 64, kStreamWaves = 8, kStreamStages = 6, kStreamCopies = 4;
 constexpr int kStreamX = kQuantBlock * kQuantBlock, kStreamS = kStreamX + kStreamRows * kQuantBlock;
 constexpr int kStreamStage = kStreamS + 4 * 256;            // scales of the rows, of the weights (64 times), bias of the 128 columns
-constexpr int kStreamMost = kStreamStages * kStreamStage, kStreamStarts = kStreamMost + kStreamWaves * kStreamRows * 4;
-constexpr int kStreamLdsBytes = kStreamStarts + (MOE_MAX_E + 1 + kStreamWaves) * 4;
+constexpr int kStreamMost = kStreamStages * kStreamStage, kStreamList = kStreamMost + kStreamWaves * kStreamRows * 4;
+constexpr int kStreamLdsBytes = kStreamList + MOE_MAX_E * 2 + kStreamWaves * 4;
 static_assert(kStreamLdsBytes <= 160 * 1024, "fits a CU");
+
+// The experts of 1 ... max_rows rows, in order, counted by every block for itself; returns how many.  `tmp`: an int per wavefront.
+template <int THREADS>
+__device__ __forceinline__ int list_experts(const QuantArgs& a, int max_rows, uint16_t* list, int32_t* tmp) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int before = 0;
+    for (int e0 = 0; e0 < a.E; e0 += THREADS) {
+        const int e = e0 + threadIdx.x;
+        const int rows = e < a.E ? segment_of(a, e).rows : 0;
+        const bool in = rows > 0 && rows <= max_rows;
+        const uint64_t ins = __ballot(in);
+        if (lane == 0) tmp[wave] = __popcll(ins);
+        __syncthreads();
+        int at = before + __popcll(ins & ((1ull << lane) - 1));
+        for (int w = 0; w < THREADS / 64; ++w) {
+            const int n = tmp[w];
+            if (w < wave) at += n;
+            before += n;
+        }
+        if (in) list[at] = static_cast<uint16_t>(e);
+        __syncthreads();
+    }
+    return __builtin_amdgcn_readfirstlane(before);
+}
 
 // OUT = kOutParts: the contraction is cut into `split` parts, whose sums go to a.out as [split][rows][pitch of N] fp32.
 constexpr int kOutParts = 3;
@@ -268,12 +333,12 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
     const int split = OUT == kOutParts ? parts_wanted : 1;
     extern __shared__ __align__(16) unsigned char smem[];
     uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kStreamMost);         // [64][8]
-    int32_t* starts = reinterpret_cast<int32_t*>(smem + kStreamStarts);
-    count_tiles<kStreamWaves * 64>(a, kStreamRows, 1, max_rows, starts, starts + MOE_MAX_E + 1);
+    uint16_t* list = reinterpret_cast<uint16_t*>(smem + kStreamList);
+    const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
-    const int per_tile = groups * split, units = starts[a.E] * per_tile;
+    const int per_tile = groups * split, units = tiles * per_tile;
 
     // Every block gets the same number of units, as few as the grid allows: a CU can pull more than its share of the memory's rate, so
     // that a quarter of them idle costs nothing, but a last round of a few units does.  The runs are dealt to the XCDs evenly.
@@ -290,11 +355,10 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
         Unit w;
         w.tile = t;
         w.rest = rest;
-        w.e = __builtin_amdgcn_readfirstlane(expert_of(starts, a.E, t));
-        const Segment seg = segment_of(a, w.e);
-        const int tile = __builtin_amdgcn_readfirstlane(t - starts[w.e]);
-        w.row0 = __builtin_amdgcn_readfirstlane(seg.row0 + tile * kStreamRows);
-        w.rows = __builtin_amdgcn_readfirstlane(min(kStreamRows, seg.rows - tile * kStreamRows));
+        w.e = __builtin_amdgcn_readfirstlane(static_cast<int>(list[t]));
+        const Segment seg = segment_of_unit(a, w.e);
+        w.row0 = seg.row0;
+        w.rows = seg.rows;
         w.group = rest / split;
         w.part = rest - w.group * split;
         w.kb = KB * w.part / split;
@@ -444,9 +508,9 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
                             const uint4 m = *reinterpret_cast<const uint4*>(mosts + (tf * 16 + r) * kStreamWaves + v);
                             most[tf] = max(most[tf], max(max(m.x, m.y), max(m.z, m.w)));
                         }
-                    store_codes(a, n0, cur.row0, cur.rows, acc, most, wave == 0);
+                    store_codes<16>(a, n0, cur.row0, cur.rows, acc, most, wave == 0);
                 } else {
-                    store_values<OUT>(a, n0, cur.row0, cur.rows, acc);
+                    store_values<OUT, 16>(a, n0, cur.row0, cur.rows, acc);
                 }
             }
         };
@@ -515,129 +579,231 @@ __global__ __launch_bounds__(256) void quant_join_kernel(const QuantArgs a, cons
 }
 
 // ---- many rows per matrix: tiles in LDS -----------------------------------------------------------------------------
-// Unit: 256 rows x 128 columns by 8 wavefronts (4 x 2, 64 x 64 each), a block of 128 columns of the contraction per step, through a
-// ring of three LDS stages: one being read, one that has landed (its first fragments are read ahead), one in flight.  Everything goes from
-// memory to LDS directly, 16 bytes per lane; a stage holds
-//   rows     [256][128 bytes]
+// Unit: 64 R rows (R = 1, 2, 4) x 128 columns by 8 wavefronts, a block of 128 columns of the contraction per step, through a ring of
+// LDS stages: one being read, one that has landed (its first fragments are read ahead), the others in flight.  Everything goes from memory
+// to LDS directly, 16 bytes per lane; a stage holds
+//   rows     [64 RMAX][128 bytes]
 //   weights  8 fragments of 2 KiB as they are packed, 16 rows each
-//   scales   of the 256 rows, and the weights' (one for the unit's 128 columns)
-constexpr int kTileRows = 256, kTileCols = kQuantBlock, kTileWaves = 8, kTileStages = 3;
-constexpr int kStageW = kTileRows * kQuantBlock, kStageS = kStageW + kTileCols * kQuantBlock, kStage = kStageS + kTileRows * 4 + 256;
-constexpr int kTileMost = kTileStages * kStage, kTileStarts = kTileMost + 2 * kTileRows * 4;
-constexpr int kTileLdsBytes = kTileStarts + (MOE_MAX_E + 1 + kTileWaves) * 4;
-static_assert(kTileLdsBytes <= 160 * 1024, "fits a CU");
+//   scales   of the rows, and the weights' (one for the unit's 128 columns)
+// Wavefront (wm, wn) of the 4 x 2 multiplies row fragments wm, wm + 4, ... (R of them) and the columns 64 wn ... 64 wn + 63.
+constexpr int kTileWaves = 8;
+template <int RMAX>
+struct Tiles {
+    static constexpr int kRows = 64 * RMAX, kStages = RMAX == 4 ? 3 : RMAX == 2 ? 4 : 6;
+    static constexpr int kStageW = kRows * kQuantBlock, kStageS = kStageW + kQuantBlock * kQuantBlock, kStage = kStageS + kRows * 4 + 256;
+    static constexpr int kMost = kStages * kStage, kStarts = kMost + 2 * kRows * 4;
+    static constexpr int kLdsBytes = kStarts + kTileWaves * 16 + (MOE_MAX_E + 1) * 4 + MOE_MAX_E * 2;
+    static constexpr int kCopies = RMAX + 3;            // a wavefront's, per stage
+    static_assert(kLdsBytes <= 160 * 1024, "fits a CU");
+};
 
-template <int OUT>
+template <int OUT, int RMAX>
 __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const QuantArgs a, int min_rows) {
+    using T = Tiles<RMAX>;
+    constexpr int kStages = T::kStages, kStageW = T::kStageW, kStageS = T::kStageS, kStage = T::kStage, tile_rows = T::kRows;
     extern __shared__ __align__(16) unsigned char smem[];
-    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kTileMost);           // [2][256]
-    int32_t* starts = reinterpret_cast<int32_t*>(smem + kTileStarts);
-    count_tiles<kTileWaves * 64>(a, kTileRows, min_rows, a.rows, starts, starts + MOE_MAX_E + 1);
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + T::kMost);           // [2][rows]
+    int4* counts = reinterpret_cast<int4*>(smem + T::kStarts);
+    int32_t* whole = reinterpret_cast<int32_t*>(counts + kTileWaves);
+    uint16_t* rest = reinterpret_cast<uint16_t*>(whole + MOE_MAX_E + 1);
+    const int last_tiles = count_tiles<kTileWaves * 64>(a, tile_rows, min_rows, whole, rest, counts);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     const int wm = wave >> 1, wn = wave & 1;
     const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
-    const int units = starts[a.E] * groups;
-    const uint32_t lds = lds_address(smem);
-    // copies: wavefront w brings rows 32 w ... 32 w + 31, weight fragment w, and the scales of rows 64 (w % 4) ... or of the weights
-    const uint32_t to_rows = lds + wave * 4096, to_weights = lds + kStageW + wave * 2048;
-    const uint32_t to_scales = lds + kStageS + (wave < 4 ? wave * 256 : kTileRows * 4);
-    const int at_x = row_operand(wm * 64), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
-    const int at_sx = kStageS + (wm * 64 + r) * 4, at_sw = kStageS + kTileRows * 4;
+    const int whole_units = whole[a.E] * groups, units = whole_units + last_tiles * groups;
+    int u = xcd_position(), u_in = u;       // the unit that is computed, and the one that is copied
+    if (u >= units) return;
 
-    for (int u = xcd_position(); u < units; u += gridDim.x) {
-        const int e = __builtin_amdgcn_readfirstlane(expert_of(starts, a.E, u / groups));
-        const int tiles = starts[e + 1] - starts[e], local = u - starts[e] * groups;
-        // eight column groups of a tile, then the next tile's: 32 neighbours share four tiles' rows and eight groups' weights
-        const int band = local / (tiles * 8), width = min(8, groups - band * 8), rest = local - band * tiles * 8;
-        const int tile = rest / width, group = band * 8 + rest % width;
-        const Segment seg = segment_of(a, e);
-        const int row0 = __builtin_amdgcn_readfirstlane(seg.row0 + tile * kTileRows);
-        const int rows = __builtin_amdgcn_readfirstlane(min(kTileRows, seg.rows - tile * kTileRows));
-        const int n0 = group * kTileCols;
-
-        const uint8_t* from_rows[4];
-        const uint8_t* from_weights = a.w + static_cast<size_t>(e) * quant_matrix_bytes(a.N, a.K) +
-                                      static_cast<size_t>(n0 / 16 + wave) * KB * kFragBytes + lane * 16;
-        const float* from_scales;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int in_tile = wave * 32 + i * 8 + (lane >> 3);
-            const size_t row = source_row(a, row0 + min(in_tile, rows - 1));
-            from_rows[i] = a.a + row * pitch + piece_of_lane(in_tile);
+    struct Unit {
+        int e, row0, rows, group;
+    };
+    auto unit_at = [&](int n) __attribute__((always_inline)) {
+        Unit w;
+        int tile;
+        if (n < whole_units) {
+            w.e = __builtin_amdgcn_readfirstlane(expert_of(whole, a.E, n / groups));
+            const int tiles = whole[w.e + 1] - whole[w.e], local = n - whole[w.e] * groups;
+            // eight column groups of a tile, then the next tile's: 32 neighbours share four tiles' rows and eight groups' weights
+            const int band = local / (tiles * 8), width = min(8, groups - band * 8), in_band = local - band * tiles * 8;
+            tile = in_band / width;
+            w.group = __builtin_amdgcn_readfirstlane(band * 8 + in_band - tile * width);
+        } else {
+            const int v = n - whole_units, t = v / groups;
+            w.e = __builtin_amdgcn_readfirstlane(static_cast<int>(rest[t]));
+            tile = whole[w.e + 1] - whole[w.e];
+            w.group = __builtin_amdgcn_readfirstlane(v - t * groups);
         }
-        if (wave < 4) from_scales = a.a_scales + static_cast<size_t>(source_row(a, row0 + min(wave * 64 + lane, rows - 1))) * KB;
-        else from_scales = a.w_scales + (static_cast<size_t>(e) * groups + group) * KB;
-        auto stage_in = [&](int slot) {
-            const int at = slot * kStage;
+        const Segment seg = segment_of_unit(a, w.e);
+        w.row0 = seg.row0 + __builtin_amdgcn_readfirstlane(tile * tile_rows);
+        w.rows = min(tile_rows, seg.rows - __builtin_amdgcn_readfirstlane(tile * tile_rows));
+        return w;
+    };
+
+    // copies: wavefront w brings rows 64 i + 8 w ... + 7, weight fragment w, and scales: of rows 64 w ... or of the weights
+    const uint32_t lds = lds_address(smem);
+    const uint32_t to_rows = lds + wave * 1024, to_weights = lds + kStageW + wave * 2048;
+    const int scale_part = wave < RMAX ? wave : RMAX;       // of 64 rows, or the weights'
+    const uint32_t to_scales = lds + kStageS + scale_part * 256;
+    const uint8_t *from_rows[RMAX], *from_weights;
+    const float* from_scales;
+    auto point_at = [&](const Unit& w) __attribute__((always_inline)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                copy16_to_lds(from_rows[i], to_rows + at + i * 1024);
-                from_rows[i] += kQuantBlock;
-            }
+        for (int i = 0; i < RMAX; ++i) {
+            const int in_tile = i * 64 + wave * 8 + (lane >> 3);
+            from_rows[i] = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(in_tile);
+        }
+        from_weights = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) +
+                       static_cast<size_t>(w.group * 8 + wave) * KB * kFragBytes + lane * 16;
+        if (scale_part < RMAX) from_scales = a.a_scales + static_cast<size_t>(source_row(a, w.row0 + min(wave * 64 + lane, w.rows - 1))) * KB;
+        else from_scales = a.w_scales + (static_cast<size_t>(w.e) * groups + w.group) * KB;
+    };
+    Unit ahead = unit_at(u_in);
+    point_at(ahead);
+    int kb_in = 0, slot_in = 0;
+    // The ring runs on across units: the next unit's first stages go out during the last steps of this one.
+    auto copy_next = [&]() __attribute__((always_inline)) {
+        const int at = slot_in * kStage;
+        slot_in = slot_in == kStages - 1 ? 0 : slot_in + 1;
+        if (u_in >= units) {               // nothing left to copy: keep up the count that the waits go by
 #pragma unroll
-            for (int i = 0; i < 2; ++i) copy16_to_lds(from_weights + i * 1024, to_weights + at + i * 1024);
-            from_weights += kFragBytes;
-            copy4_to_lds(from_scales, to_scales + at);
+            for (int i = 0; i < T::kCopies; ++i) copy4_to_lds(from_scales, to_scales + at);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < RMAX; ++i) {
+            copy16_to_lds(from_rows[i], to_rows + at + i * 8192);
+            from_rows[i] += kQuantBlock;
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) copy16_to_lds(from_weights + i * 1024, to_weights + at + i * 1024);
+        from_weights += kFragBytes;
+        copy4_to_lds(from_scales, to_scales + at);
+        if (++kb_in < KB) {
             ++from_scales;
-        };
-        f32x4 acc[4][4];
+        } else {
+            kb_in = 0;
+            u_in += gridDim.x;
+            if (u_in < units) {
+                ahead = unit_at(u_in);
+                point_at(ahead);
+            }
+        }
+    };
+    Unit cur = ahead;
+    copy_next();
+    copies_landed<0>();
+#pragma unroll 1
+    for (int i = 0; i < kStages - 2; ++i) copy_next();
+
+    const int at_x = row_operand(wm * 16), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
+    const int at_sx = kStageS + (wm * 16 + r) * 4, at_sw = kStageS + tile_rows * 4;
+    auto row_codes = [&](const unsigned char* st, int i) { return read_codes(st + at_x + i * 64 * kQuantBlock, x_other); };
+    auto weight_codes = [&](const unsigned char* st, int nf) { return read_codes(st + at_w + nf * kFragBytes, 1024); };
+    int slot = 0;
+    auto run_unit = [&](auto fragments) __attribute__((always_inline)) {
+        constexpr int R = decltype(fragments)::value;
+        // At the beginning of a step: w[0], w[1] and the first row fragment widened, the codes of w[2], w[3] and of the second row
+        // fragment (if there is one).
+        Widened w[4], x;
+        i32x8 codes_w[2], codes_x;
+        const unsigned char* st0 = smem + slot * kStage;
+        w[0] = widen(weight_codes(st0, 0));
+        w[1] = widen(weight_codes(st0, 1));
+        codes_w[0] = weight_codes(st0, 2);
+        codes_w[1] = weight_codes(st0, 3);
+        x = widen(row_codes(st0, 0));
+        codes_x = row_codes(st0, 1);
+        f32x4 acc[4][R];
 #pragma unroll
         for (int nf = 0; nf < 4; ++nf)
 #pragma unroll
-            for (int tf = 0; tf < 4; ++tf) acc[nf][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-        copies_landed<0>();         // the ring is free
-        stage_in(0);
-        if (KB > 1) stage_in(1);
-        if (KB > 1) copies_landed<7>();
-        else copies_landed<0>();
-        Widened w[4];
-#pragma unroll
-        for (int nf = 0; nf < 4; ++nf) w[nf] = widen(read_codes(smem + at_w + nf * kFragBytes, 1024));
-        i32x8 x = read_codes(smem + at_x, x_other);
-        int slot = 0;
+            for (int i = 0; i < R; ++i) acc[nf][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
         for (int j = 0; j < KB; ++j) {
-            const int next = slot == kTileStages - 1 ? 0 : slot + 1, after = next == kTileStages - 1 ? 0 : next + 1;
             const unsigned char* st = smem + slot * kStage;
-            const unsigned char* st_next = smem + next * kStage;
-            const bool more = j + 1 < KB;
-            if (more) copies_landed<0>();
-            if (j + 2 < KB) stage_in(after);
+            slot = slot == kStages - 1 ? 0 : slot + 1;
+            const unsigned char* st_next = smem + slot * kStage;
+            float scale[R];
             const float sw = *reinterpret_cast<const float*>(st + at_sw);
 #pragma unroll
-            for (int tf = 0; tf < 4; ++tf) {
-                const float scale = *reinterpret_cast<const float*>(st + at_sx + tf * 64) * sw;
-                const Widened wx = widen(x);
-                if (tf < 3) x = read_codes(st + at_x + (tf + 1) * kFragBytes, x_other);
-                else if (more) x = read_codes(st_next + at_x, x_other);
+            for (int i = 0; i < R; ++i) scale[i] = *reinterpret_cast<const float*>(st + at_sx + i * 256) * sw;
 #pragma unroll
-                for (int nf = 0; nf < 4; ++nf) {
-                    const f32x4 p = mfma_block(w[nf], wx);
-                    if (tf == 3 && more) w[nf] = widen(read_codes(st_next + at_w + nf * kFragBytes, 1024));
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[nf][tf][i] = fmaf(scale, p[i], acc[nf][tf][i]);
+            for (int i = 0; i < R; ++i) {
+                if (i == (R > 2 ? R - 2 : 0)) {            // the next stage has landed, the one after it goes out
+                    __builtin_amdgcn_sched_barrier(0);
+                    copies_landed<(kStages - 3) * T::kCopies>();
+                    copy_next();
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                // the next row fragment is widened meanwhile, the codes of the one after it are read; behind the last one comes the next
+                // stage's first
+                if (R == 1) codes_x = row_codes(st_next, 0);
+                const i32x8 later_codes = i + 2 < R ? row_codes(st, i + 2) : row_codes(st_next, i + 2 == R ? 0 : 1);
+                i32x8 next_w[2];
+                if (i == R - 1) {
+                    next_w[0] = weight_codes(st_next, 0);
+                    next_w[1] = weight_codes(st_next, 1);
+                }
+                Widened later;
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    if (i == 0 && half == 0 && R == 1) {
+                        w[2] = widen(codes_w[0]);
+                        w[3] = widen(codes_w[1]);
+                    }
+                    f32x4 p[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+                            p[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2 * half + q].v[k], x.v[k], p[q], 0, 0, 0);
+                    widen_half(codes_x, half, later);
+                    if (i == 0 && half == 0 && R > 1) {
+                        w[2] = widen(codes_w[0]);
+                        w[3] = widen(codes_w[1]);
+                    }
+                    if (i == R - 1 && half == 1) {
+                        w[0] = widen(next_w[0]);
+                        w[1] = widen(next_w[1]);
+                        codes_w[0] = weight_codes(st_next, 2);
+                        codes_w[1] = weight_codes(st_next, 3);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) acc[2 * half + q][i][k] = fmaf(scale[i], p[q][k], acc[2 * half + q][i][k]);
+                }
+                x = later;
+                codes_x = later_codes;
             }
-            slot = next;
         }
-        const int col0 = n0 + wn * 64, first = wm * 64;            // this wavefront's columns and rows
-        finish_values(a, e, col0, acc);
+        const int col0 = cur.group * kQuantBlock + wn * 64, first = wm * 16;            // this wavefront's columns and rows
+        finish_values(a, cur.e, col0, acc);
         if constexpr (OUT == kOutE4m3) {
-            uint32_t most[4];
+            uint32_t most[R];
             row_magnitudes(a.N, col0, acc, most);
             if (lane < 16) {
 #pragma unroll
-                for (int tf = 0; tf < 4; ++tf) mosts[wn * kTileRows + first + tf * 16 + lane] = most[tf];
+                for (int i = 0; i < R; ++i) mosts[wn * tile_rows + first + i * 64 + lane] = most[i];
             }
-            __syncthreads();
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-            for (int tf = 0; tf < 4; ++tf) most[tf] = max(most[tf], mosts[(wn ^ 1) * kTileRows + first + tf * 16 + r]);
-            store_codes(a, col0, row0 + first, rows - first, acc, most, wn == 0);
+            for (int i = 0; i < R; ++i) most[i] = max(most[i], mosts[(wn ^ 1) * tile_rows + first + i * 64 + r]);
+            store_codes<64>(a, col0, cur.row0 + first, cur.rows - first, acc, most, wn == 0);
         } else {
-            store_values<OUT>(a, col0, row0 + first, rows - first, acc);
+            store_values<OUT, 64>(a, col0, cur.row0 + first, cur.rows - first, acc);
         }
+    };
+    while (true) {
+        if (RMAX == 1 || cur.rows <= 64) run_unit(std::integral_constant<int, 1>{});
+        else if (RMAX == 2 || cur.rows <= 128) run_unit(std::integral_constant<int, (RMAX < 2 ? RMAX : 2)>{});
+        else run_unit(std::integral_constant<int, RMAX>{});
+        u += gridDim.x;
+        if (u >= units) break;
+        cur = unit_at(u);
     }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
@@ -659,9 +825,28 @@ size_t quant_product_workspace(const moe_quant_shape& s) {
     return (std::max<size_t>(parts, 1) + 255) / 256 * 256;
 }
 
+// Row fragments per wavefront of the tiled kernel, so rows per tile / 64: large tiles do more per byte and per conversion, small ones
+// occupy more CUs.  A step of 256, 128 and 64 rows takes 2.06, 1.2 and 0.83 us on a CU; a unit of each kind has as many steps as the
+// other, so what counts is rounds of 256 units times that.  (1501 rows x 768 x 3072 54.6, 37.0 and 27.9 us; 16384 x 8192 x 2048 542, 671
+// and 988.)  A grouped call's last tiles are not known here and left out.
+static int tile_fragments(int rows, int N) {
+    auto cost = [&](int r, float step) {
+        const long long units = static_cast<long long>((rows + 64 * r - 1) / (64 * r)) * quant_blocks(N);
+        return static_cast<float>((units + 255) / 256) * step;
+    };
+    const float c4 = cost(4, 2.06f), c2 = cost(2, 1.2f), c1 = cost(1, 0.83f);
+    return c1 < c2 && c1 < c4 ? 1 : c2 < c4 ? 2 : 4;
+}
+
+template <int OUT, int RMAX>
+static void launch_tiles(const QuantArgs& a, int grid, hipStream_t stream) {
+    quant_tile_kernel<OUT, RMAX><<<dim3(grid), dim3(kTileWaves * 64), Tiles<RMAX>::kLdsBytes, stream>>>(a, kTiledMinRows);
+}
+
 template <int OUT>
 static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
-    const dim3 grid(device_cu_count()), threads(kStreamWaves * 64);
+    const int cus = device_cu_count();
+    const dim3 grid(cus), threads(kStreamWaves * 64);
     const int split = stream_split(a.rows, a.N, a.K, a.E);
     if (split > 1) {
         QuantArgs parts = a;
@@ -670,7 +855,12 @@ static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
         quant_join_kernel<OUT><<<dim3(a.rows, (quant_blocks(a.N) + 7) / 8), dim3(256), 0, stream>>>(a, static_cast<const float*>(ws), split);
         return hipGetLastError();
     }
-    if (a.rows >= kTiledMinRows) quant_tile_kernel<OUT><<<grid, dim3(kTileWaves * 64), kTileLdsBytes, stream>>>(a, kTiledMinRows);
+    if (a.rows >= kTiledMinRows) {
+        const int r = tile_fragments(a.rows, a.N);
+        if (r == 4) launch_tiles<OUT, 4>(a, cus, stream);
+        else if (r == 2) launch_tiles<OUT, 2>(a, cus, stream);
+        else launch_tiles<OUT, 1>(a, cus, stream);
+    }
     if (a.offsets != nullptr || a.rows < kTiledMinRows)
         quant_stream_kernel<OUT><<<grid, threads, kStreamLdsBytes, stream>>>(a, std::min(a.rows, kTiledMinRows - 1), 1);
     return hipGetLastError();
@@ -680,9 +870,15 @@ hipError_t configure_quant_kernels() {
     const struct {
         const void* kernel;
         int lds;
-    } all[] = {{reinterpret_cast<const void*>(quant_tile_kernel<kOutF32>), kTileLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16>), kTileLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3>), kTileLdsBytes},
+    } all[] = {{reinterpret_cast<const void*>(quant_tile_kernel<kOutF32, 4>), Tiles<4>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutF32, 2>), Tiles<2>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutF32, 1>), Tiles<1>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16, 4>), Tiles<4>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16, 2>), Tiles<2>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16, 1>), Tiles<1>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3, 4>), Tiles<4>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3, 2>), Tiles<2>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3, 1>), Tiles<1>::kLdsBytes},
                {reinterpret_cast<const void*>(quant_stream_kernel<kOutF32>), kStreamLdsBytes},
                {reinterpret_cast<const void*>(quant_stream_kernel<kOutBf16>), kStreamLdsBytes},
                {reinterpret_cast<const void*>(quant_stream_kernel<kOutE4m3>), kStreamLdsBytes},
