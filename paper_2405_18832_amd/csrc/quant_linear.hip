@@ -16,29 +16,19 @@ enum OutKind { kOutF32 = 0, kOutBf16 = 1, kOutE4m3 = 2 };
 
 // 32 codes of a lane as bf16 values, which hold them exactly.
 struct Widened {
-    bf16x8 v[4];
+    i32x4 v[4];
+    __device__ __forceinline__ bf16x8 eight(int i) const { return __builtin_bit_cast(bf16x8, v[i]); }
+    // the values of codes 2 n, 2 n + 1, in the four bytes that hold them
+    __device__ __forceinline__ void widen_two(int32_t codes, int n) {
+        v[n >> 2][n & 3] = __builtin_bit_cast(int32_t, n & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, true)
+                                                              : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
+    }
 };
-__device__ __forceinline__ bf16x8 widen8(int32_t lo, int32_t hi) {
-    union {
-        bf16x2_t two[4];
-        bf16x8 eight;
-    } u;
-    u.two[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
-    u.two[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
-    u.two[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
-    u.two[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
-    return u.eight;
-}
 __device__ __forceinline__ Widened widen(const i32x8& codes) {
     Widened r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) r.v[i] = widen8(codes[2 * i], codes[2 * i + 1]);
+    for (int n = 0; n < 16; ++n) r.widen_two(codes[n >> 1], n);
     return r;
-}
-// Half of them: the values of codes 16 half ... 16 half + 15.
-__device__ __forceinline__ void widen_half(const i32x8& codes, int half, Widened& r) {
-#pragma unroll
-    for (int i = 2 * half; i < 2 * half + 2; ++i) r.v[i] = widen8(codes[2 * i], codes[2 * i + 1]);
 }
 
 // 16 x 16 results of one block of 128 columns: first operand 16 weight rows, second 16 token rows.  Lane l holds 32 codes of row
@@ -49,7 +39,7 @@ __device__ __forceinline__ void widen_half(const i32x8& codes, int half, Widened
 __device__ __forceinline__ f32x4 mfma_block(const Widened& w, const Widened& x) {
     f32x4 p = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.v[i], x.v[i], p, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.eight(i), x.eight(i), p, 0, 0, 0);
     return p;
 }
 
@@ -57,6 +47,21 @@ __device__ __forceinline__ float quant_activate(float v, int act) {
     if (act == MOE_ACT_GELU) return gelu_exp(v);
     if (act == MOE_ACT_RELU) return v < 0.f ? 0.f : v;      // NaN stays
     return v;
+}
+
+// A value whose uses are computed where they stand: what is needed once per unit is not to be kept in registers through the steps.
+__device__ __forceinline__ int here(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
+// The same value for the whole wavefront, told to the compiler where it cannot see it.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+template <typename P>
+__device__ __forceinline__ const P* uniform(const P* p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    return reinterpret_cast<const P*>(static_cast<uint64_t>(static_cast<uint32_t>(uniform(static_cast<int>(v)))) |
+                                      static_cast<uint64_t>(static_cast<uint32_t>(uniform(static_cast<int>(v >> 32)))) << 32);
 }
 
 // ---- which rows are whose -------------------------------------------------------------------------------------------
@@ -172,7 +177,7 @@ __device__ __forceinline__ void activate_values(int act, f32x4 (&acc)[NF][TF]) {
 }
 template <int NF, int TF>
 __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0, f32x4 (&acc)[NF][TF]) {
-    const int g = (threadIdx.x & 63) >> 4;
+    const int g = (here(threadIdx.x) & 63) >> 4;
 #pragma unroll
     for (int nf = 0; nf < NF; ++nf) {
         const int n = n0 + nf * 16 + g * 4;
@@ -192,7 +197,7 @@ __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0,
 template <int OUT, int STRIDE, int NF, int TF>
 __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row0, int rows, const f32x4 (&acc)[NF][TF]) {
     static_assert(OUT != kOutE4m3, "");
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int lane = here(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
     // four columns at once where every row begins on a boundary of four
     const bool wide = a.N % 4 == 0 && reinterpret_cast<uintptr_t>(a.out) % (OUT == kOutF32 ? 16 : 8) == 0;
 #pragma unroll
@@ -222,7 +227,7 @@ __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row
 // Largest magnitude of each row over the wavefront's columns that exist, for lane l of row 16 tf + l % 16.
 template <int NF, int TF>
 __device__ __forceinline__ void row_magnitudes(int N, int n0, f32x4 (&acc)[NF][TF], uint32_t (&most)[TF]) {
-    const int g = (threadIdx.x & 63) >> 4;
+    const int g = (here(threadIdx.x) & 63) >> 4;
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
         uint32_t m = 0;
@@ -243,7 +248,7 @@ __device__ __forceinline__ void row_magnitudes(int N, int n0, f32x4 (&acc)[NF][T
 template <int STRIDE, int NF, int TF>
 __device__ __forceinline__ void store_codes(const QuantArgs& a, int n0, int row0, int rows, const f32x4 (&acc)[NF][TF],
                                             const uint32_t (&most)[TF], bool scales) {
-    const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int lane = here(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
     const size_t pitch = quant_pitch(a.N);
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
@@ -269,6 +274,15 @@ __device__ __forceinline__ void copy4_to_lds(const void* src, uint32_t lds_base)
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(dst) : "memory");
 }
+// The same from 32-bit offsets to a base that is the same for the whole wavefront: half the registers, and the base moves on for free
+__device__ __forceinline__ void copy16_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
+}
+__device__ __forceinline__ void copy4_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
+}
 // The wavefront's copies up to the newest `left` have landed, and with the barrier everybody's; every LDS read before it is done too.
 template <int LEFT>
 __device__ __forceinline__ void copies_landed() {
@@ -281,7 +295,7 @@ __device__ __forceinline__ i32x8 read_codes(const unsigned char* p, int other) {
 }
 // Rows in LDS: 128 bytes each, the 16-byte pieces of a row permuted by its number, so that an operand read (16 rows x one piece) meets no
 // bank twice: piece c of row r lies at c ^ (r / 2 % 8).  A copy brings 8 rows, each a whole line by eight lanes.
-__device__ __forceinline__ int piece_of_lane(int row) { return ((threadIdx.x & 7) ^ (row >> 1 & 7)) << 4; }
+__device__ __forceinline__ int piece_of_lane(int lane, int row) { return ((lane & 7) ^ (row >> 1 & 7)) << 4; }
 // Where lane l reads piece l / 16 of row `first` + l % 16 (`first` a multiple of 16), and how far from there piece 4 + l / 16 lies.
 __device__ __forceinline__ int row_operand(int first) {
     const int lane = threadIdx.x & 63, r = lane & 15;
@@ -384,7 +398,7 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
     int scales_step;
     auto point_at_tile = [&](const Unit& w) __attribute__((always_inline)) {
         const int in_tile = wave * 8 + (lane >> 3);
-        tile_row = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(in_tile);
+        tile_row = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(lane, in_tile);
         tile_scale = a.a_scales + static_cast<size_t>(source_row(a, w.row0 + min(lane, w.rows - 1))) * KB;
     };
     auto point_at = [&](const Unit& w) __attribute__((always_inline)) {
@@ -611,7 +625,7 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
     const int wm = wave >> 1, wn = wave & 1;
     const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
-    const int whole_units = whole[a.E] * groups, units = whole_units + last_tiles * groups;
+    const int whole_units = __builtin_amdgcn_readfirstlane(whole[a.E]) * groups, units = whole_units + last_tiles * groups;
     int u = xcd_position(), u_in = u;       // the unit that is computed, and the one that is copied
     if (u >= units) return;
 
@@ -623,7 +637,8 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         int tile;
         if (n < whole_units) {
             w.e = __builtin_amdgcn_readfirstlane(expert_of(whole, a.E, n / groups));
-            const int tiles = whole[w.e + 1] - whole[w.e], local = n - whole[w.e] * groups;
+            const int before = __builtin_amdgcn_readfirstlane(whole[w.e]);
+            const int tiles = __builtin_amdgcn_readfirstlane(whole[w.e + 1]) - before, local = n - before * groups;
             // eight column groups of a tile, then the next tile's: 32 neighbours share four tiles' rows and eight groups' weights
             const int band = local / (tiles * 8), width = min(8, groups - band * 8), in_band = local - band * tiles * 8;
             tile = in_band / width;
@@ -631,7 +646,7 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         } else {
             const int v = n - whole_units, t = v / groups;
             w.e = __builtin_amdgcn_readfirstlane(static_cast<int>(rest[t]));
-            tile = whole[w.e + 1] - whole[w.e];
+            tile = __builtin_amdgcn_readfirstlane(whole[w.e + 1] - whole[w.e]);
             w.group = __builtin_amdgcn_readfirstlane(v - t * groups);
         }
         const Segment seg = segment_of_unit(a, w.e);
@@ -645,50 +660,76 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
     const uint32_t to_rows = lds + wave * 1024, to_weights = lds + kStageW + wave * 2048;
     const int scale_part = wave < RMAX ? wave : RMAX;       // of 64 rows, or the weights'
     const uint32_t to_scales = lds + kStageS + scale_part * 256;
-    const uint8_t *from_rows[RMAX], *from_weights;
-    const float* from_scales;
+    // Of a stage: the row pieces' offsets from `rows_base` (tiles of 256 rows have no registers for whole addresses; see tile_fragments for
+    // operands of more than 4 GiB), the weights' and scales' base.
+    constexpr bool OFFSETS = RMAX == 4;
+    uint32_t row_offset[OFFSETS ? RMAX : 1], scale_offset = 0;
+    const uint8_t* row_from[OFFSETS ? 1 : RMAX];
+    const uint8_t *rows_base = a.a, *weights_base = a.w;
+    const float *scales_base = a.a_scales, *scales_from = nullptr;
+    const uint32_t lane16 = lane * 16;
     auto point_at = [&](const Unit& w) __attribute__((always_inline)) {
+        const int lane = here(threadIdx.x) & 63;
 #pragma unroll
         for (int i = 0; i < RMAX; ++i) {
             const int in_tile = i * 64 + wave * 8 + (lane >> 3);
-            from_rows[i] = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(in_tile);
+            const int row = source_row(a, w.row0 + min(in_tile, w.rows - 1));
+            if constexpr (OFFSETS) row_offset[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(pitch) + piece_of_lane(lane, in_tile);
+            else row_from[i] = a.a + row * pitch + piece_of_lane(lane, in_tile);
         }
-        from_weights = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) +
-                       static_cast<size_t>(w.group * 8 + wave) * KB * kFragBytes + lane * 16;
-        if (scale_part < RMAX) from_scales = a.a_scales + static_cast<size_t>(source_row(a, w.row0 + min(wave * 64 + lane, w.rows - 1))) * KB;
-        else from_scales = a.w_scales + (static_cast<size_t>(w.e) * groups + w.group) * KB;
+        rows_base = a.a;
+        weights_base = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) + static_cast<size_t>(w.group * 8 + wave) * KB * kFragBytes;
+        const int scale_row = scale_part < RMAX ? source_row(a, w.row0 + min(wave * 64 + lane, w.rows - 1)) : 0;
+        const float* base = scale_part < RMAX ? a.a_scales : a.w_scales + (static_cast<size_t>(w.e) * groups + w.group) * KB;
+        if constexpr (OFFSETS) {
+            scales_base = base;
+            scale_offset = static_cast<uint32_t>(scale_row) * static_cast<uint32_t>(KB * 4);
+        } else {
+            scales_from = base + static_cast<size_t>(scale_row) * KB;
+        }
     };
     Unit ahead = unit_at(u_in);
     point_at(ahead);
     int kb_in = 0, slot_in = 0;
-    // The ring runs on across units: the next unit's first stages go out during the last steps of this one.
-    auto copy_next = [&]() __attribute__((always_inline)) {
+    // The ring runs on across units: the next unit's first stages go out during the last steps of this one.  Behind the last unit the
+    // last stage is copied again, which keeps up the count that the waits go by.
+    auto copy_piece = [&](int n) __attribute__((always_inline)) {
         const int at = slot_in * kStage;
+        if (n < RMAX) {
+            if constexpr (OFFSETS) copy16_to_lds(rows_base, row_offset[n < RMAX ? n : 0], to_rows + at + n * 8192);
+            else copy16_to_lds(row_from[n < RMAX ? n : 0], to_rows + at + n * 8192);
+        } else if (n < RMAX + 2) {
+            copy16_to_lds(weights_base + (n - RMAX) * 1024, lane16, to_weights + at + (n - RMAX) * 1024);
+        } else if (n == RMAX + 2) {
+            if constexpr (OFFSETS) copy4_to_lds(scales_base, scale_offset, to_scales + at);
+            else copy4_to_lds(scales_from, to_scales + at);
+        }
+    };
+    auto next_stage = [&]() __attribute__((always_inline)) {
         slot_in = slot_in == kStages - 1 ? 0 : slot_in + 1;
-        if (u_in >= units) {               // nothing left to copy: keep up the count that the waits go by
-#pragma unroll
-            for (int i = 0; i < T::kCopies; ++i) copy4_to_lds(from_scales, to_scales + at);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < RMAX; ++i) {
-            copy16_to_lds(from_rows[i], to_rows + at + i * 8192);
-            from_rows[i] += kQuantBlock;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) copy16_to_lds(from_weights + i * 1024, to_weights + at + i * 1024);
-        from_weights += kFragBytes;
-        copy4_to_lds(from_scales, to_scales + at);
         if (++kb_in < KB) {
-            ++from_scales;
-        } else {
+            weights_base += kFragBytes;
+            if constexpr (OFFSETS) {
+                rows_base += kQuantBlock;
+                ++scales_base;
+            } else {
+#pragma unroll
+                for (int i = 0; i < RMAX; ++i) row_from[i] += kQuantBlock;
+                ++scales_from;
+            }
+        } else if (u_in + static_cast<int>(gridDim.x) < units) {
             kb_in = 0;
             u_in += gridDim.x;
-            if (u_in < units) {
-                ahead = unit_at(u_in);
-                point_at(ahead);
-            }
+            ahead = unit_at(u_in);
+            point_at(ahead);
+        } else {
+            kb_in = KB - 1;
         }
+    };
+    auto copy_next = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < T::kCopies; ++n) copy_piece(n);
+        next_stage();
     };
     Unit cur = ahead;
     copy_next();
@@ -699,26 +740,36 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
     const int at_x = row_operand(wm * 16), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
     const int at_sx = kStageS + (wm * 16 + r) * 4, at_sw = kStageS + tile_rows * 4;
     auto row_codes = [&](const unsigned char* st, int i) { return read_codes(st + at_x + i * 64 * kQuantBlock, x_other); };
+    auto row_codes_half = [&](const unsigned char* st, int i, int half) {
+        return *reinterpret_cast<const i32x4*>(st + at_x + i * 64 * kQuantBlock + (half ? x_other : 0));
+    };
     auto weight_codes = [&](const unsigned char* st, int nf) { return read_codes(st + at_w + nf * kFragBytes, 1024); };
     int slot = 0;
     auto run_unit = [&](auto fragments) __attribute__((always_inline)) {
         constexpr int R = decltype(fragments)::value;
-        // At the beginning of a step: w[0], w[1] and the first row fragment widened, the codes of w[2], w[3] and of the second row
-        // fragment (if there is one).
-        Widened w[4], x;
-        i32x8 codes_w[2], codes_x;
-        const unsigned char* st0 = smem + slot * kStage;
-        w[0] = widen(weight_codes(st0, 0));
-        w[1] = widen(weight_codes(st0, 1));
-        codes_w[0] = weight_codes(st0, 2);
-        codes_w[1] = weight_codes(st0, 3);
-        x = widen(row_codes(st0, 0));
-        codes_x = row_codes(st0, 1);
         f32x4 acc[4][R];
 #pragma unroll
         for (int nf = 0; nf < 4; ++nf)
 #pragma unroll
             for (int i = 0; i < R; ++i) acc[nf][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // A step is 2 R rounds of eight matrix instructions, two weight fragments x one row fragment.  What the vector unit has to do
+        // is spread between them, one piece after each: the codes of the next row fragment are widened, the sums of the round before
+        // are added to the accumulators; in the last round and in the next step's first one also the next stage's weights are widened,
+        // two fragments each, as their registers fall free.  The order is held by the scheduling barriers.
+        // At the beginning of a step: w[0], w[1] and the first row fragment widened, the codes of w[2], w[3] and half of the
+        // second row fragment's (if there is one), and the sums of the last round before it.
+        Widened w[4], x[2];
+        i32x8 codes_w[2], next_w[2];
+        i32x4 codes_x[2];                   // halves of the fragment that is widened next
+        f32x4 sums[2][2] = {};
+        float last_scale = 0.f;
+        const unsigned char* st0 = smem + slot * kStage;
+        w[0] = widen(weight_codes(st0, 0));
+        w[1] = widen(weight_codes(st0, 1));
+        codes_w[0] = weight_codes(st0, 2);
+        codes_w[1] = weight_codes(st0, 3);
+        x[0] = widen(row_codes(st0, 0));
+        codes_x[0] = row_codes_half(st0, 1, 0);
 #pragma unroll 1
         for (int j = 0; j < KB; ++j) {
             const unsigned char* st = smem + slot * kStage;
@@ -727,57 +778,65 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
             float scale[R];
             const float sw = *reinterpret_cast<const float*>(st + at_sw);
 #pragma unroll
-            for (int i = 0; i < R; ++i) scale[i] = *reinterpret_cast<const float*>(st + at_sx + i * 256) * sw;
+            for (int i = 0; i < R; ++i) scale[i] = *reinterpret_cast<const float*>(st + at_sx + i * 256);
 #pragma unroll
-            for (int i = 0; i < R; ++i) {
-                if (i == (R > 2 ? R - 2 : 0)) {            // the next stage has landed, the one after it goes out
+            for (int round = 0; round < 2 * R; ++round) {
+                const int i = round >> 1, half = round & 1;
+                if (round == (R > 2 ? 2 * R - 4 : 0)) {     // the next stage has landed, the one after it goes out
                     __builtin_amdgcn_sched_barrier(0);
                     copies_landed<(kStages - 3) * T::kCopies>();
-                    copy_next();
-                    __builtin_amdgcn_sched_barrier(0);
+                    if (R == 1) codes_x[0] = row_codes_half(st_next, 0, 0);
                 }
-                // the next row fragment is widened meanwhile, the codes of the one after it are read; behind the last one comes the next
-                // stage's first
-                if (R == 1) codes_x = row_codes(st_next, 0);
-                const i32x8 later_codes = i + 2 < R ? row_codes(st, i + 2) : row_codes(st_next, i + 2 == R ? 0 : 1);
-                i32x8 next_w[2];
-                if (i == R - 1) {
+                // A round ahead of its use: the second half of the fragment that is widened now, the first half of the one after it.
+                // Behind the last row fragment comes the next stage's first.
+                if (half == 0) codes_x[1] = i + 1 < R ? row_codes_half(st, i + 1, 1) : row_codes_half(st_next, 0, 1);
+                else if (R > 1) codes_x[0] = i + 2 < R ? row_codes_half(st, i + 2, 0) : row_codes_half(st_next, i + 2 - R, 0);
+                if (half == 0 && i == R - 1) {
                     next_w[0] = weight_codes(st_next, 0);
                     next_w[1] = weight_codes(st_next, 1);
                 }
-                Widened later;
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    if (i == 0 && half == 0 && R == 1) {
-                        w[2] = widen(codes_w[0]);
-                        w[3] = widen(codes_w[1]);
-                    }
-                    f32x4 p[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-#pragma unroll
-                        for (int q = 0; q < 2; ++q)
-                            p[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2 * half + q].v[k], x.v[k], p[q], 0, 0, 0);
-                    widen_half(codes_x, half, later);
-                    if (i == 0 && half == 0 && R > 1) {
-                        w[2] = widen(codes_w[0]);
-                        w[3] = widen(codes_w[1]);
-                    }
-                    if (i == R - 1 && half == 1) {
-                        w[0] = widen(next_w[0]);
-                        w[1] = widen(next_w[1]);
-                        codes_w[0] = weight_codes(st_next, 2);
-                        codes_w[1] = weight_codes(st_next, 3);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 2; ++q)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) acc[2 * half + q][i][k] = fmaf(scale[i], p[q][k], acc[2 * half + q][i][k]);
+                if (R == 1 && round == 1) {                 // one row fragment: their last use was a round ago
+                    w[2] = widen(codes_w[0]);
+                    w[3] = widen(codes_w[1]);
                 }
-                x = later;
-                codes_x = later_codes;
+                Widened& x_now = x[R > 1 ? i & 1 : 0];
+                Widened& x_later = x[R > 1 ? (i & 1) ^ 1 : 1];
+                const int before = round == 0 ? 2 * R - 1 : round - 1;      // the round whose sums are added
+                const float by = round == 0 ? last_scale : scale[before >> 1] * sw;
+#pragma unroll
+                for (int m = 0; m < 8; ++m) {
+                    const int k = m >> 1, q = m & 1;
+                    f32x4& p = sums[round & 1][q];
+                    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2 * half + q].eight(k), x_now.eight(k),
+                                                                k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p, 0, 0, 0);
+                    // one copy at a time: issued together they would hold up every wavefront
+                    constexpr int kFirst = R > 2 ? 8 * (2 * R - 4) : 0, kEvery = R == 1 ? 2 : 4;
+                    const int at = 8 * round + m - kFirst;
+                    if (at >= 0 && at % kEvery == 0) copy_piece(at / kEvery);
+                    x_later.widen_two(codes_x[half][m >> 1], half * 8 + m);
+                    f32x4& sum = acc[2 * (before & 1) + (m >> 2)][before >> 1];
+                    sum[m & 3] = fmaf(by, sums[(round & 1) ^ 1][m >> 2][m & 3], sum[m & 3]);
+                    if (R > 1 && round == 0) {
+#pragma unroll
+                        for (int c = 4 * m; c < 4 * m + 4; ++c) w[2 + (c >> 4)].widen_two(codes_w[c >> 4][(c & 15) >> 1], c & 15);
+                    }
+                    if (round == 2 * R - 1) {
+#pragma unroll
+                        for (int c = 4 * m; c < 4 * m + 4; ++c) w[c >> 4].widen_two(next_w[c >> 4][(c & 15) >> 1], c & 15);
+                        if (m == 4) codes_w[0] = weight_codes(st_next, 2);
+                        if (m == 7) codes_w[1] = weight_codes(st_next, 3);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
+            next_stage();
+            last_scale = scale[R - 1] * sw;
+            if (R == 1) x[0] = x[1];
         }
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+            acc[2 + (m >> 2)][R - 1][m & 3] = fmaf(last_scale, sums[1][m >> 2][m & 3], acc[2 + (m >> 2)][R - 1][m & 3]);
+        const int lane = here(threadIdx.x) & 63, r = lane & 15;
         const int col0 = cur.group * kQuantBlock + wn * 64, first = wm * 16;            // this wavefront's columns and rows
         finish_values(a, cur.e, col0, acc);
         if constexpr (OUT == kOutE4m3) {
@@ -799,7 +858,17 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         if (RMAX == 1 || cur.rows <= 64) run_unit(std::integral_constant<int, 1>{});
         else if (RMAX == 2 || cur.rows <= 128) run_unit(std::integral_constant<int, (RMAX < 2 ? RMAX : 2)>{});
         else run_unit(std::integral_constant<int, RMAX>{});
-        u += gridDim.x;
+        // behind the stores, which not every lane does, and three ways to get here
+        u_in = uniform(u_in);
+        kb_in = uniform(kb_in);
+        slot_in = uniform(slot_in);
+        slot = uniform(slot);
+        weights_base = uniform(weights_base);
+        if constexpr (OFFSETS) {
+            rows_base = uniform(rows_base);
+            scales_base = uniform(scales_base);
+        }
+        u = uniform(u + static_cast<int>(gridDim.x));
         if (u >= units) break;
         cur = unit_at(u);
     }
@@ -826,16 +895,17 @@ size_t quant_product_workspace(const moe_quant_shape& s) {
 }
 
 // Row fragments per wavefront of the tiled kernel, so rows per tile / 64: large tiles do more per byte and per conversion, small ones
-// occupy more CUs.  A step of 256, 128 and 64 rows takes 2.06, 1.2 and 0.83 us on a CU; a unit of each kind has as many steps as the
-// other, so what counts is rounds of 256 units times that.  (1501 rows x 768 x 3072 54.6, 37.0 and 27.9 us; 16384 x 8192 x 2048 542, 671
-// and 988.)  A grouped call's last tiles are not known here and left out.
-static int tile_fragments(int rows, int N) {
+// occupy more CUs.  A step of 256, 128 and 64 rows takes 1.95, 1.2 and 0.8 us on a CU; a unit of each kind has as many steps as the
+// other, so what counts is rounds of 256 units times that.  (1501 rows x 768 x 3072 54.6, 37.0 and 26.2 us; 16384 x 8192 x 2048 542, 671
+// and 988.)  A grouped call's last tiles are not known here and left out.  Tiles of 256 rows address the rows by 32-bit offsets.
+static int tile_fragments(int rows, int N, size_t operand_bytes) {
     auto cost = [&](int r, float step) {
         const long long units = static_cast<long long>((rows + 64 * r - 1) / (64 * r)) * quant_blocks(N);
         return static_cast<float>((units + 255) / 256) * step;
     };
-    const float c4 = cost(4, 2.06f), c2 = cost(2, 1.2f), c1 = cost(1, 0.83f);
-    return c1 < c2 && c1 < c4 ? 1 : c2 < c4 ? 2 : 4;
+    const float c4 = cost(4, 1.95f), c2 = cost(2, 1.2f), c1 = cost(1, 0.8f);
+    if (c1 < c2 && c1 < c4) return 1;
+    return c2 < 0.9f * c4 || operand_bytes > 0xffffffffull ? 2 : 4;
 }
 
 template <int OUT, int RMAX>
@@ -856,7 +926,7 @@ static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
         return hipGetLastError();
     }
     if (a.rows >= kTiledMinRows) {
-        const int r = tile_fragments(a.rows, a.N);
+        const int r = tile_fragments(a.rows, a.N, a.rows / a.k * quant_pitch(a.K));
         if (r == 4) launch_tiles<OUT, 4>(a, cus, stream);
         else if (r == 2) launch_tiles<OUT, 2>(a, cus, stream);
         else launch_tiles<OUT, 1>(a, cus, stream);
