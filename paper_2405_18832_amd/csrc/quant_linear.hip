@@ -277,11 +277,11 @@ __device__ __forceinline__ void copy4_to_lds(const void* src, uint32_t lds_base)
 // The same from 32-bit offsets to a base that is the same for the whole wavefront: half the registers, and the base moves on for free
 __device__ __forceinline__ void copy16_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(offset), "s"(uniform(static_cast<const char*>(base))), "s"(dst) : "memory");
 }
 __device__ __forceinline__ void copy4_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(base), "s"(dst) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(offset), "s"(uniform(static_cast<const char*>(base))), "s"(dst) : "memory");
 }
 // The wavefront's copies up to the newest `left` have landed, and with the barrier everybody's; every LDS read before it is done too.
 template <int LEFT>
@@ -297,8 +297,8 @@ __device__ __forceinline__ i32x8 read_codes(const unsigned char* p, int other) {
 // bank twice: piece c of row r lies at c ^ (r / 2 % 8).  A copy brings 8 rows, each a whole line by eight lanes.
 __device__ __forceinline__ int piece_of_lane(int lane, int row) { return ((lane & 7) ^ (row >> 1 & 7)) << 4; }
 // Where lane l reads piece l / 16 of row `first` + l % 16 (`first` a multiple of 16), and how far from there piece 4 + l / 16 lies.
-__device__ __forceinline__ int row_operand(int first) {
-    const int lane = threadIdx.x & 63, r = lane & 15;
+__device__ __forceinline__ int row_operand(int tid, int first) {
+    const int lane = tid & 63, r = lane & 15;
     return (first + r) * kQuantBlock + (((lane >> 4) ^ (r >> 1)) << 4);
 }
 __device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 : 64; }
@@ -460,7 +460,7 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
     for (int i = 0; i < kStreamStages - 1; ++i) copy_next();
 
     Unit cur = unit_at(tile0, first - tile0 * per_tile);
-    const int at_w = wave * kFragBytes + lane * 16, at_x = kStreamX + row_operand(0), x_other = row_operand_other(at_x);
+    const int at_w = wave * kFragBytes + lane * 16, at_x = kStreamX + row_operand(threadIdx.x, 0), x_other = row_operand_other(at_x);
     const int at_sx = kStreamS + r * 4, at_sw = kStreamS + 256, at_bias = kStreamS + 512 + (wave * 16 + (lane >> 4) * 4) * 4;
     int slot = 0;
     while (true) {
@@ -705,31 +705,44 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
             else copy4_to_lds(scales_from, to_scales + at);
         }
     };
+    uint32_t stage_step = 1;               // 0 behind the last unit
     auto next_stage = [&]() __attribute__((always_inline)) {
         slot_in = slot_in == kStages - 1 ? 0 : slot_in + 1;
-        if (++kb_in < KB) {
-            weights_base += kFragBytes;
-            if constexpr (OFFSETS) {
-                rows_base += kQuantBlock;
-                ++scales_base;
-            } else {
+        weights_base += stage_step * kFragBytes;
+        if constexpr (OFFSETS) {
+            rows_base += stage_step * kQuantBlock;
+            scales_base += stage_step;
+        } else {
 #pragma unroll
-                for (int i = 0; i < RMAX; ++i) row_from[i] += kQuantBlock;
-                ++scales_from;
-            }
-        } else if (u_in + static_cast<int>(gridDim.x) < units) {
-            kb_in = 0;
+            for (int i = 0; i < RMAX; ++i) row_from[i] += stage_step * kQuantBlock;
+            scales_from += stage_step;
+        }
+    };
+    // when all of a unit's stages have been sent for (kb_in == KB)
+    auto next_unit = [&]() __attribute__((always_inline)) {
+        kb_in = 0;
+        if (u_in + static_cast<int>(gridDim.x) < units) {
             u_in += gridDim.x;
             ahead = unit_at(u_in);
             point_at(ahead);
-        } else {
-            kb_in = KB - 1;
+        } else if (stage_step != 0) {      // back to the last stage, which is copied from now on
+            weights_base -= kFragBytes;
+            if constexpr (OFFSETS) {
+                rows_base -= kQuantBlock;
+                --scales_base;
+            } else {
+#pragma unroll
+                for (int i = 0; i < RMAX; ++i) row_from[i] -= kQuantBlock;
+                --scales_from;
+            }
+            stage_step = 0;
         }
     };
     auto copy_next = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < T::kCopies; ++n) copy_piece(n);
         next_stage();
+        if (++kb_in == KB) next_unit();
     };
     Unit cur = ahead;
     copy_next();
@@ -737,16 +750,17 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
 #pragma unroll 1
     for (int i = 0; i < kStages - 2; ++i) copy_next();
 
-    const int at_x = row_operand(wm * 16), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes + lane * 16;
-    const int at_sx = kStageS + (wm * 16 + r) * 4, at_sw = kStageS + tile_rows * 4;
-    auto row_codes = [&](const unsigned char* st, int i) { return read_codes(st + at_x + i * 64 * kQuantBlock, x_other); };
-    auto row_codes_half = [&](const unsigned char* st, int i, int half) {
-        return *reinterpret_cast<const i32x4*>(st + at_x + i * 64 * kQuantBlock + (half ? x_other : 0));
-    };
-    auto weight_codes = [&](const unsigned char* st, int nf) { return read_codes(st + at_w + nf * kFragBytes, 1024); };
     int slot = 0;
     auto run_unit = [&](auto fragments) __attribute__((always_inline)) {
         constexpr int R = decltype(fragments)::value;
+        const int tid = here(threadIdx.x);
+        const int at_x = row_operand(tid, wm * 16), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes;
+        const int at_sx = kStageS + (wm * 16 + (tid & 15)) * 4, at_sw = kStageS + tile_rows * 4;
+        auto row_codes = [&](const unsigned char* st, int i) { return read_codes(st + at_x + i * 64 * kQuantBlock, x_other); };
+        auto row_codes_half = [&](const unsigned char* st, int i, int half) {
+            return *reinterpret_cast<const i32x4*>(st + at_x + i * 64 * kQuantBlock + (half ? x_other : 0));
+        };
+        auto weight_codes = [&](const unsigned char* st, int nf) { return read_codes(st + at_w + lane16 + nf * kFragBytes, 1024); };
         f32x4 acc[4][R];
 #pragma unroll
         for (int nf = 0; nf < 4; ++nf)
@@ -770,8 +784,25 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         codes_w[1] = weight_codes(st0, 3);
         x[0] = widen(row_codes(st0, 0));
         codes_x[0] = row_codes_half(st0, 1, 0);
+        // the steps to the end of the unit or to where the copies go on to the next one: without a branch, so that the order stays
 #pragma unroll 1
-        for (int j = 0; j < KB; ++j) {
+        for (int j = 0; j < KB;) {
+        // behind branches that not every lane takes, such as the stores of the unit before
+        u_in = uniform(u_in);
+        kb_in = uniform(kb_in);
+        slot_in = uniform(slot_in);
+        slot = uniform(slot);
+        stage_step = uniform(stage_step);
+        weights_base = uniform(weights_base);
+        if constexpr (OFFSETS) {
+            rows_base = uniform(rows_base);
+            scales_base = uniform(scales_base);
+        }
+        const int steps = min(KB - j, KB - kb_in);
+        j += steps;
+        kb_in += steps;
+#pragma unroll 1
+        for (int s = 0; s < steps; ++s) {
             const unsigned char* st = smem + slot * kStage;
             slot = slot == kStages - 1 ? 0 : slot + 1;
             const unsigned char* st_next = smem + slot * kStage;
@@ -833,6 +864,8 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
             last_scale = scale[R - 1] * sw;
             if (R == 1) x[0] = x[1];
         }
+        if (kb_in == KB) next_unit();
+        }
 #pragma unroll
         for (int m = 0; m < 8; ++m)
             acc[2 + (m >> 2)][R - 1][m & 3] = fmaf(last_scale, sums[1][m >> 2][m & 3], acc[2 + (m >> 2)][R - 1][m & 3]);
@@ -858,16 +891,6 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         if (RMAX == 1 || cur.rows <= 64) run_unit(std::integral_constant<int, 1>{});
         else if (RMAX == 2 || cur.rows <= 128) run_unit(std::integral_constant<int, (RMAX < 2 ? RMAX : 2)>{});
         else run_unit(std::integral_constant<int, RMAX>{});
-        // behind the stores, which not every lane does, and three ways to get here
-        u_in = uniform(u_in);
-        kb_in = uniform(kb_in);
-        slot_in = uniform(slot_in);
-        slot = uniform(slot);
-        weights_base = uniform(weights_base);
-        if constexpr (OFFSETS) {
-            rows_base = uniform(rows_base);
-            scales_base = uniform(scales_base);
-        }
         u = uniform(u + static_cast<int>(gridDim.x));
         if (u >= units) break;
         cur = unit_at(u);
