@@ -343,9 +343,8 @@ __device__ __forceinline__ int list_experts(const QuantArgs& a, int max_rows, ui
 constexpr int kOutParts = 3;
 
 template <int OUT>
-__global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
+__device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, int parts_wanted, int b, unsigned char* smem) {
     const int split = OUT == kOutParts ? parts_wanted : 1;
-    extern __shared__ __align__(16) unsigned char smem[];
     uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kStreamMost);         // [64][8]
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + kStreamList);
     const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
@@ -357,7 +356,7 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
     // Every block gets the same number of units, as few as the grid allows: a CU can pull more than its share of the memory's rate, so
     // that a quarter of them idle costs nothing, but a last round of a few units does.  The runs are dealt to the XCDs evenly.
     const int G = gridDim.x, rounds = (units + G - 1) / G, runs = rounds > 0 ? (units + rounds - 1) / rounds : 0;
-    const int per_xcd = (runs + 7) >> 3, b = blockIdx.x;
+    const int per_xcd = (runs + 7) >> 3;
     const int run = G % 8 == 0 ? (b >> 3 < per_xcd ? (b & 7) * per_xcd + (b >> 3) : runs) : b;
     const int first = run * rounds, last = min(units, first + rounds);
     if (first >= last) return;
@@ -538,31 +537,39 @@ __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const Q
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
 }
 
+template <int OUT>
+__global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    stream_units<OUT>(a, max_rows, parts_wanted, blockIdx.x, smem);
+}
+
 // Adds up the parts of a split contraction, in their order, and finishes the rows.  A block of threads per row and 8 groups of 128
 // columns; four columns per thread.
 template <int OUT>
 __global__ __launch_bounds__(256) void quant_join_kernel(const QuantArgs a, const float* __restrict__ parts, int split) {
     const int row = blockIdx.x, lane = threadIdx.x & 63;
-    __shared__ int32_t before;
-    int e = 0;
-    if (a.offsets != nullptr) {            // the expert whose rows this one is among
-        if (threadIdx.x == 0) before = 0;
-        __syncthreads();
-        int n = 0;
-        for (int i = threadIdx.x; i < a.E; i += 256) n += a.offsets[i + 1] <= row ? 1 : 0;
-        atomicAdd(&before, n);
-        __syncthreads();
-        e = before;
-        if (e >= a.E) return;
-        const Segment seg = segment_of(a, e);
-        if (row < seg.row0 || row >= seg.row0 + seg.rows) return;
-    }
     const int n0 = (blockIdx.y * 256 + threadIdx.x) * 4;
     const size_t pitch = quant_pitch(a.N);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (n0 < static_cast<int>(pitch)) {
         const float* p = parts + static_cast<size_t>(row) * pitch + n0;
-        for (int s = 0; s < split; ++s) v += *reinterpret_cast<const f32x4*>(p + static_cast<size_t>(s) * a.rows * pitch);
+        const size_t stride = static_cast<size_t>(a.rows) * pitch;
+        int s = 0;
+        for (; s + 4 <= split; s += 4) {
+            f32x4 part[4];                 // four loads in flight, added in the parts' order
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[i] = *reinterpret_cast<const f32x4*>(p + (s + i) * stride);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v += part[i];
+        }
+        for (; s < split; ++s) v += *reinterpret_cast<const f32x4*>(p + s * stride);
+    }
+    int e = 0;
+    if (a.offsets != nullptr) {            // the expert whose rows this one is among: as many end at or before it as precede that
+        for (int e0 = 0; e0 < a.E; e0 += 256) e += __syncthreads_count(e0 + static_cast<int>(threadIdx.x) < a.E && a.offsets[e0 + threadIdx.x + 1] <= row);
+        if (e >= a.E) return;
+        const Segment seg = segment_of(a, e);
+        if (row < seg.row0 || row >= seg.row0 + seg.rows) return;
     }
     uint32_t most = 0;
 #pragma unroll
@@ -612,10 +619,9 @@ struct Tiles {
 };
 
 template <int OUT, int RMAX>
-__global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const QuantArgs a, int min_rows) {
+__device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, unsigned char* smem) {
     using T = Tiles<RMAX>;
     constexpr int kStages = T::kStages, kStageW = T::kStageW, kStageS = T::kStageS, kStage = T::kStage, tile_rows = T::kRows;
-    extern __shared__ __align__(16) unsigned char smem[];
     uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + T::kMost);           // [2][rows]
     int4* counts = reinterpret_cast<int4*>(smem + T::kStarts);
     int32_t* whole = reinterpret_cast<int32_t*>(counts + kTileWaves);
@@ -895,7 +901,18 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_tile_kernel(const Quant
         if (u >= units) break;
         cur = unit_at(u);
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is used for something else by then
+}
+
+// Both kinds of units of a grouped product as one kernel, the tiles first: where one kind does not occur, a launch of its own would
+// cost 4 to 5 us all the same.  The blocks that have a tile more are the last ones to get a run of streamed units.
+template <int OUT, int RMAX>
+__global__ __launch_bounds__(kTileWaves * 64) void quant_product_kernel(const QuantArgs a, int tiled_min_rows) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    tile_units<OUT, RMAX>(a, tiled_min_rows, smem);
+    if (a.offsets == nullptr) return;
+    __syncthreads();
+    stream_units<OUT>(a, tiled_min_rows - 1, 1, gridDim.x - 1 - blockIdx.x, smem);
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
@@ -931,9 +948,13 @@ static int tile_fragments(int rows, int N, size_t operand_bytes) {
     return c2 < 0.9f * c4 || operand_bytes > 0xffffffffull ? 2 : 4;
 }
 
+// dynamic LDS of the kernel with both kinds of units
+template <int RMAX>
+constexpr int kProductLds = Tiles<RMAX>::kLdsBytes > kStreamLdsBytes ? Tiles<RMAX>::kLdsBytes : kStreamLdsBytes;
+
 template <int OUT, int RMAX>
 static void launch_tiles(const QuantArgs& a, int grid, hipStream_t stream) {
-    quant_tile_kernel<OUT, RMAX><<<dim3(grid), dim3(kTileWaves * 64), Tiles<RMAX>::kLdsBytes, stream>>>(a, kTiledMinRows);
+    quant_product_kernel<OUT, RMAX><<<dim3(grid), dim3(kTileWaves * 64), kProductLds<RMAX>, stream>>>(a, kTiledMinRows);
 }
 
 template <int OUT>
@@ -953,9 +974,9 @@ static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
         if (r == 4) launch_tiles<OUT, 4>(a, cus, stream);
         else if (r == 2) launch_tiles<OUT, 2>(a, cus, stream);
         else launch_tiles<OUT, 1>(a, cus, stream);
+    } else {
+        quant_stream_kernel<OUT><<<grid, threads, kStreamLdsBytes, stream>>>(a, a.rows, 1);
     }
-    if (a.offsets != nullptr || a.rows < kTiledMinRows)
-        quant_stream_kernel<OUT><<<grid, threads, kStreamLdsBytes, stream>>>(a, std::min(a.rows, kTiledMinRows - 1), 1);
     return hipGetLastError();
 }
 
@@ -963,15 +984,15 @@ hipError_t configure_quant_kernels() {
     const struct {
         const void* kernel;
         int lds;
-    } all[] = {{reinterpret_cast<const void*>(quant_tile_kernel<kOutF32, 4>), Tiles<4>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutF32, 2>), Tiles<2>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutF32, 1>), Tiles<1>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16, 4>), Tiles<4>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16, 2>), Tiles<2>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutBf16, 1>), Tiles<1>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3, 4>), Tiles<4>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3, 2>), Tiles<2>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_tile_kernel<kOutE4m3, 1>), Tiles<1>::kLdsBytes},
+    } all[] = {{reinterpret_cast<const void*>(quant_product_kernel<kOutF32, 4>), kProductLds<4>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutF32, 2>), kProductLds<2>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutF32, 1>), kProductLds<1>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutBf16, 4>), kProductLds<4>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutBf16, 2>), kProductLds<2>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutBf16, 1>), kProductLds<1>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 4>), kProductLds<4>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 2>), kProductLds<2>},
+               {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 1>), kProductLds<1>},
                {reinterpret_cast<const void*>(quant_stream_kernel<kOutF32>), kStreamLdsBytes},
                {reinterpret_cast<const void*>(quant_stream_kernel<kOutBf16>), kStreamLdsBytes},
                {reinterpret_cast<const void*>(quant_stream_kernel<kOutE4m3>), kStreamLdsBytes},
