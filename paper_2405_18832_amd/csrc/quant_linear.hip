@@ -24,6 +24,13 @@ struct Widened {
                                                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, 1.f, false));
     }
 };
+// the values of codes 8 k ... 8 k + 7
+__device__ __forceinline__ bf16x8 widen8(const i32x8& codes, int k) {
+    Widened r;
+#pragma unroll
+    for (int n = 4 * k; n < 4 * k + 4; ++n) r.widen_two(codes[n >> 1], n);
+    return r.eight(k);
+}
 __device__ __forceinline__ Widened widen(const i32x8& codes) {
     Widened r;
 #pragma unroll
@@ -31,18 +38,11 @@ __device__ __forceinline__ Widened widen(const i32x8& codes) {
     return r;
 }
 
-// 16 x 16 results of one block of 128 columns: first operand 16 weight rows, second 16 token rows.  Lane l holds 32 codes of row
-// l % 16 of each; which columns they are does not matter as long as both operands agree (moe.h: 64 h + 16 (l / 16), h = 0, 1).
-// Result i of lane l: weight row 4 (l / 16) + i, token row l % 16.
-// On the bf16 units: those for 8-bit operands (v_mfma_f32_16x16x128_f8f6f4) add up groups of products after aligning them to the largest
-// and drop what lies below about 2^-14 of it, which is 1.5e-5 of the rms of a sum of 128 products of normal values.
-__device__ __forceinline__ f32x4 mfma_block(const Widened& w, const Widened& x) {
-    f32x4 p = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w.eight(i), x.eight(i), p, 0, 0, 0);
-    return p;
-}
-
+// The matrix instruction's first operand is 16 weight rows, the second one 16 token rows.  Lane l holds 32 codes of row l % 16 of each;
+// which columns they are does not matter as long as both operands agree (moe.h: 64 h + 16 (l / 16), h = 0, 1).  Result i of lane l: weight
+// row 4 (l / 16) + i, token row l % 16.  The bf16 units are used: those for 8-bit operands (v_mfma_f32_16x16x128_f8f6f4) add up groups of
+// products after aligning them to the largest and drop what lies below about 2^-14 of it, which is 1.5e-5 of the rms of a sum of 128
+// products of normal values.
 __device__ __forceinline__ float quant_activate(float v, int act) {
     if (act == MOE_ACT_GELU) return gelu_exp(v);
     if (act == MOE_ACT_RELU) return v < 0.f ? 0.f : v;      // NaN stays
@@ -471,24 +471,32 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
             f32x4 bias = {0.f, 0.f, 0.f, 0.f};
             for (; cur.kb < cur.kb1; ++cur.kb) {
                 copies_landed<(kStreamStages - 2) * kStreamCopies>();
-                copy_next();
                 const unsigned char* st = smem + slot * kStreamStage;
+                const i32x8 w = read_codes(st + at_w, 1024);
                 const float sw = *reinterpret_cast<const float*>(st + at_sw);
-                const Widened w = widen(read_codes(st + at_w, 1024));
                 i32x8 x[TF];
                 float sx[TF];
 #pragma unroll
-                for (int tf = 0; tf < TF; ++tf) {
-                    x[tf] = read_codes(st + at_x + tf * kFragBytes, x_other);
-                    sx[tf] = *reinterpret_cast<const float*>(st + at_sx + tf * 64);
+                for (int tf = 0; tf < TF; ++tf) x[tf] = read_codes(st + at_x + tf * kFragBytes, x_other);
+#pragma unroll
+                for (int tf = 0; tf < TF; ++tf) sx[tf] = *reinterpret_cast<const float*>(st + at_sx + tf * 64);
+                if constexpr (OUT != kOutParts) bias = *reinterpret_cast<const f32x4*>(st + at_bias);
+                copy_next();
+                // a quarter of the block after the other, so that the row fragments' sums are independent of each other and codes are
+                // widened while others are multiplied
+                f32x4 p[TF];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bf16x8 wide = widen8(w, k);
+#pragma unroll
+                    for (int tf = 0; tf < TF; ++tf)
+                        p[tf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, widen8(x[tf], k), k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p[tf], 0, 0, 0);
                 }
-                if (cur.kb + 1 == cur.kb1) bias = *reinterpret_cast<const f32x4*>(st + at_bias);
 #pragma unroll
                 for (int tf = 0; tf < TF; ++tf) {
-                    const f32x4 p = mfma_block(w, widen(x[tf]));
                     const float scale = sx[tf] * sw;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[0][tf][i] = fmaf(scale, p[i], acc[0][tf][i]);
+                    for (int i = 0; i < 4; ++i) acc[0][tf][i] = fmaf(scale, p[tf][i], acc[0][tf][i]);
                 }
                 slot = slot == kStreamStages - 1 ? 0 : slot + 1;
             }
@@ -530,6 +538,7 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
         const int tf = (cur.rows + 15) >> 4;
         if (tf == 1) run_unit(std::integral_constant<int, 1>{});
         else if (tf == 2) run_unit(std::integral_constant<int, 2>{});
+        else if (tf == 3) run_unit(std::integral_constant<int, 3>{});
         else run_unit(std::integral_constant<int, 4>{});
         if (--units_out == 0) break;
         cur = cur.rest + 1 == per_tile ? unit_at(cur.tile + 1, 0) : along(cur);
