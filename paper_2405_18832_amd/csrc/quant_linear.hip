@@ -101,6 +101,7 @@ __device__ __forceinline__ int count_tiles(const QuantArgs& a, int tile_rows, in
     // the lengths' totals are needed before the first expert's place is known: first pass counts, second one places
     for (int pass = 0; pass < 2; ++pass) {
         if (pass == 1) {
+            if (before.x + before.y + before.z + before.w == 0) break;         // the same for every thread
             kind_base[1] = before.y;
             kind_base[2] = before.y + before.z;
             if (threadIdx.x == 0) whole[a.E] = before.x;
@@ -133,6 +134,8 @@ __device__ __forceinline__ int count_tiles(const QuantArgs& a, int tile_rows, in
             __syncthreads();
         }
     }
+    if (before.x + before.y + before.z + before.w == 0 && threadIdx.x == 0) whole[a.E] = 0;
+    __syncthreads();
     return __builtin_amdgcn_readfirstlane(before.y + before.z + before.w);
 }
 // The expert that tile t of a list belongs to: the last whose tiles begin at or before t.  By whole wavefronts.
@@ -929,12 +932,13 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_product_kernel(const Qu
 constexpr int kTiledMinRows = 65;
 
 // Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave most CUs without one.
-// A grouped call's number of row tiles is not known here; half of the most it can be is taken.
+// It costs a second launch: one to four parts of 64 units 14.7 -> 12.4 us (32 x 8192 x 2048), of 16 units to sixteen 13.7 -> 11.3 us
+// (1 x 2048 x 8192); but 128 units 13.3 -> 14.5 us with two (the experts of one token, 8192 x 2048).
+// A grouped call's number of experts with rows is not known here; a row each is taken, the most it can be.
 static int stream_split(int rows, int N, int K, int E) {
     if (rows >= kTiledMinRows) return 1;
-    const int tiles = E == 1 ? 1 : (std::min(rows, E) + 1) / 2;
-    const int units = tiles * quant_blocks(N);
-    return std::max(1, std::min(256 / units, quant_blocks(K) / 2));
+    const int units = std::min(rows, E) * quant_blocks(N);
+    return units <= 96 ? std::max(1, std::min(256 / units, quant_blocks(K) / 2)) : 1;
 }
 
 size_t quant_product_workspace(const moe_quant_shape& s) {

@@ -1,0 +1,144 @@
+"""Feed-forward blocks in 8 bits, as a pre-norm model runs them: their tensors on the device and the calls into the C ABI.
+
+`QuantMoEBlock`: residual addition and RMS norm with a quantised output, routing on the norm in bf16, both expert products on e4m3 rows
+and weights, combine.  `QuantDenseBlock`: the same for the dense layers between the expert layers.  No arithmetic happens here.
+
+    block = QuantMoEBlock(T, d_model, d_ff, E, k, w1, w2, w_gate, norm_weight)      # w1 [E, d_ff, d_model], w2 [E, d_model, d_ff]
+    y, stream = block.forward(x, residual)     # stream = x + residual continues; y is the next block's x
+
+Both products of a step of T tokens use workspaces that are made once; a block of another T shares the weights through `resized`.
+"""
+from __future__ import annotations
+
+import copy
+from typing import Optional
+
+import torch
+
+from . import (make_quant_shape, make_shape, moe_combine, moe_norm_quantize, moe_permute, moe_quant_expert_linear, moe_quant_linear,
+               moe_quant_pitch, moe_quant_weight_bytes, moe_quant_workspace_bytes, moe_quantize_weights, moe_route, moe_workspace_bytes)
+
+_DTYPES = {torch.float32: "f32", torch.bfloat16: "bf16", torch.float8_e4m3fn: "e4m3"}
+
+
+def _blocks(n: int) -> int:
+    return moe_quant_pitch(n) // 128
+
+
+class QuantWeights:
+    """E matrices [E, N, K] in the products' layout and their scales.  `w`: fp32 or bf16 weights, which are quantised, or a checkpoint's
+    e4m3 codes with their `scales` [E, ceil(N / 128), ceil(K / 128)]."""
+
+    def __init__(self, w: torch.Tensor, scales: Optional[torch.Tensor] = None):
+        self.E, self.N, self.K = w.shape
+        if (w.dtype == torch.float8_e4m3fn) != (scales is not None):
+            raise ValueError("scales belong to e4m3 codes")
+        if scales is not None and tuple(scales.shape) != (self.E, _blocks(self.N), _blocks(self.K)):
+            raise ValueError("one scale per matrix and 128 x 128 block")
+        self.codes = torch.empty(moe_quant_weight_bytes(self.E, self.N, self.K), dtype=torch.uint8, device=w.device)
+        self.scales = scales.float().contiguous() if scales is not None else torch.empty(
+            (self.E, _blocks(self.N), _blocks(self.K)), device=w.device)
+        moe_quantize_weights(self.E, self.N, self.K, _DTYPES[w.dtype], w, self.codes, None if scales is not None else self.scales)
+
+
+class _Rows:
+    """Quantised rows [R, C]."""
+
+    def __init__(self, R: int, C: int, device):
+        self.codes = torch.empty((R, moe_quant_pitch(C)), dtype=torch.float8_e4m3fn, device=device)
+        self.scales = torch.empty((R, _blocks(C)), device=device)
+
+
+class _Block:
+    def _norm_buffers(self, norm_out: bool):
+        d, dev = self.d_model, self.device
+        self.stream = torch.empty((self.T, d), dtype=torch.bfloat16, device=dev)
+        self.normed = torch.empty((self.T, d), dtype=torch.bfloat16, device=dev) if norm_out else None
+        self.x8 = _Rows(self.T, d, dev)
+        self.out = torch.empty((self.T, d), dtype=torch.bfloat16, device=dev)
+
+    def _norm(self, x, residual):
+        moe_norm_quantize(self.T, self.d_model, "bf16", x, residual, self.norm_weight, self.eps, self.stream, self.normed, self.x8.codes,
+                          self.x8.scales)
+
+    def _workspace(self, shape):
+        return torch.empty(moe_quant_workspace_bytes(shape), dtype=torch.uint8, device=self.device)
+
+    def resized(self, T: int):
+        """The same block for T tokens: weights shared, buffers of its own."""
+        other = copy.copy(self)
+        other.T = T
+        other._buffers()
+        return other
+
+
+class QuantMoEBlock(_Block):
+    def __init__(self, T, d_model, d_ff, E, k, w1, w2, w_gate, norm_weight=None, *, w1_scales=None, w2_scales=None, gate_bias=None, b1=None,
+                 b2=None, activation="relu", renormalize=True, eps=1e-6):
+        self.T, self.d_model, self.d_ff, self.E, self.k = T, d_model, d_ff, E, k
+        self.device, self.eps, self.activation, self.renormalize = w1.device, eps, activation, renormalize
+        self.w1, self.w2 = QuantWeights(w1, w1_scales), QuantWeights(w2, w2_scales)
+        if (self.w1.E, self.w1.N, self.w1.K) != (E, d_ff, d_model) or (self.w2.E, self.w2.N, self.w2.K) != (E, d_model, d_ff):
+            raise ValueError("w1 is [E, d_ff, d_model], w2 [E, d_model, d_ff]")
+        self.w_gate, self.gate_bias, self.norm_weight, self.b1, self.b2 = w_gate, gate_bias, norm_weight, b1, b2
+        self._buffers()
+
+    def _buffers(self):
+        T, k, E, dev = self.T, self.k, self.E, self.device
+        A = T * k
+        self._norm_buffers(norm_out=True)
+        self.layer = make_shape(T, self.d_model, self.d_ff, E, k, "bf16", self.renormalize)
+        self.first = make_quant_shape(A, self.d_ff, self.d_model, E, k, self.activation, "e4m3")
+        self.second = make_quant_shape(A, self.d_model, self.d_ff, E, 1, "none", "f32")
+        i32 = torch.int32
+        self.topk_idx = torch.empty((T, k), dtype=i32, device=dev)
+        self.topk_w = torch.empty((T, k), device=dev)
+        self.counts = torch.empty(E, dtype=i32, device=dev)
+        self.offsets = torch.empty(E + 1, dtype=i32, device=dev)
+        self.perm, self.inv_perm = (torch.empty(A, dtype=i32, device=dev) for _ in range(2))
+        self.hot_mask = torch.empty(E, dtype=torch.uint8, device=dev)
+        self.h8 = _Rows(A, self.d_ff, dev)
+        self.y_perm = torch.empty((A, self.d_model), device=dev)
+        self.ws = torch.empty(max(256, moe_workspace_bytes(self.layer)), dtype=torch.uint8, device=dev)
+        self.ws1, self.ws2 = self._workspace(self.first), self._workspace(self.second)
+
+    def forward(self, x, residual=None, H: int = -1):
+        """(the block's output, the residual stream x + residual), both [T, d_model] bf16 and overwritten by the next call.  H >= 0: the
+        share of the H experts with the most tokens."""
+        self._norm(x, residual)
+        mask = self.hot_mask if H >= 0 else None
+        moe_route(self.layer, self.normed, self.w_gate, self.gate_bias, self.topk_idx, self.topk_w, None, self.counts, self.offsets, H, mask,
+                  self.ws)
+        moe_permute(self.layer, None, self.topk_idx, self.offsets, self.perm, self.inv_perm, None, self.ws)
+        moe_quant_expert_linear(self.first, self.x8.codes, self.x8.scales, self.perm, self.offsets, mask, self.w1.codes, self.w1.scales, self.b1,
+                                self.h8.codes, self.h8.scales, self.ws1)
+        moe_quant_expert_linear(self.second, self.h8.codes, self.h8.scales, None, self.offsets, mask, self.w2.codes, self.w2.scales, self.b2,
+                                self.y_perm, None, self.ws2)
+        moe_combine(self.layer, self.y_perm, self.inv_perm, self.topk_idx, self.topk_w, mask, self.out)
+        return self.out, self.stream
+
+
+class QuantDenseBlock(_Block):
+    def __init__(self, T, d_model, d_ff, w1, w2, norm_weight=None, *, w1_scales=None, w2_scales=None, b1=None, b2=None, activation="relu",
+                 eps=1e-6):
+        self.T, self.d_model, self.d_ff = T, d_model, d_ff
+        self.device, self.eps, self.activation, self.norm_weight, self.b1, self.b2 = w1.device, eps, activation, norm_weight, b1, b2
+        one = lambda t: None if t is None else t[None]
+        self.w1, self.w2 = QuantWeights(w1[None], one(w1_scales)), QuantWeights(w2[None], one(w2_scales))
+        if (self.w1.N, self.w1.K) != (d_ff, d_model) or (self.w2.N, self.w2.K) != (d_model, d_ff):
+            raise ValueError("w1 is [d_ff, d_model], w2 [d_model, d_ff]")
+        self._buffers()
+
+    def _buffers(self):
+        self._norm_buffers(norm_out=False)
+        self.first = make_quant_shape(self.T, self.d_ff, self.d_model, 1, 1, self.activation, "e4m3")
+        self.second = make_quant_shape(self.T, self.d_model, self.d_ff, 1, 1, "none", "bf16")
+        self.h8 = _Rows(self.T, self.d_ff, self.device)
+        self.ws1, self.ws2 = self._workspace(self.first), self._workspace(self.second)
+
+    def forward(self, x, residual=None):
+        """(the block's output, the residual stream x + residual), both [T, d_model] bf16 and overwritten by the next call."""
+        self._norm(x, residual)
+        moe_quant_linear(self.first, self.x8.codes, self.x8.scales, self.w1.codes, self.w1.scales, self.b1, self.h8.codes, self.h8.scales, self.ws1)
+        moe_quant_linear(self.second, self.h8.codes, self.h8.scales, self.w2.codes, self.w2.scales, self.b2, self.out, None, self.ws2)
+        return self.out, self.stream

@@ -442,3 +442,119 @@ def test_in_a_graph(gpu_lib):
         steps(*want)
         torch.cuda.synchronize()
         assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+
+
+# ---- the blocks that run them together -----------------------------------------------------------------------------
+def block_inputs(T, d, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    new = lambda *s: torch.randn(s, device="cuda", generator=gen)
+    return gen, new, new(T, d).bfloat16(), (3 * new(T, d)).bfloat16()
+
+
+def check_norm(block, x, residual, d):
+    total = wl.round_to_storage(x.float().cpu().numpy() + residual.float().cpu().numpy(), "bf16").astype(np.float64)
+    assert np.array_equal(block.stream.float().cpu().numpy(), total)
+    ref = qo.norm(total, block.norm_weight.cpu().numpy().astype(np.float64), block.eps)
+    assert_codes(codes_of(block.x8.codes), block.x8.scales.cpu().numpy().astype(np.float64), ref, NORM * np.abs(ref), d)
+    return ref
+
+
+def unpacked(weights, e):
+    """Values of matrix e of QuantWeights, from the codes in the products' layout."""
+    N, K = weights.N, weights.K
+    nb, kb = qo.blocks(N) * 8, qo.blocks(K)
+    codes = weights.codes.view(weights.E, -1)[e].cpu().numpy().reshape(nb, kb, 2, 4, 16, 16).transpose(0, 4, 1, 2, 3, 5).reshape(nb * 16, kb * 128)
+    return VALUES[codes[:N, :K]] * qo.spread(weights.scales[e].cpu().numpy().astype(np.float64), N, K)
+
+
+def row_values(rows, C):
+    return qo.dequantize_rows(VALUES[codes_of(rows.codes)[:, :C]], rows.scales.cpu().numpy().astype(np.float64))
+
+
+@pytest.mark.parametrize("T,d,f,E,k,H,act", [(1, 256, 512, 16, 2, -1, "relu"), (33, 96, 160, 5, 1, -1, "gelu"), (700, 256, 384, 6, 2, -1, "relu"),
+                                             (300, 128, 256, 40, 2, 3, "relu")])
+def test_moe_block(gpu_lib, T, d, f, E, k, H, act):
+    """Every step of the block against the reference on what the step before left on the device."""
+    from oracle import moe_oracle as orc
+    from paper_2405_18832_amd.quant_layer import QuantMoEBlock
+    say(f"[case] QuantMoEBlock T={T} d={d} f={f} E={E} k={k} H={H} {act}")
+    gen, new, x, r = block_inputs(T, d, T + d)
+    w1, w2 = (new(E, f, d) / d ** 0.5).bfloat16(), (new(E, d, f) / f ** 0.5).bfloat16()
+    bias = 0.3 * new(E) if H >= 0 else None
+    block = QuantMoEBlock(T, d, f, E, k, w1, w2, (0.3 * new(E, d)).bfloat16(), torch.exp(0.2 * new(d)), gate_bias=bias, b1=0.3 * new(E, f),
+                          b2=0.3 * new(E, d), activation=act)
+    block.y_perm.fill_(float("nan"))
+    out, stream = block.forward(x, r, H)
+    torch.cuda.synchronize()
+    assert out is block.out and stream is block.stream
+    ref = check_norm(block, x, r, d)
+    normed = block.normed.float().cpu().numpy()
+    assert (np.abs(normed - ref) <= (HALF["bf16"] + NORM) * np.abs(ref) * 1.001).all()
+    route = orc.route(normed, block.w_gate.float().cpu().numpy(), None if bias is None else bias.cpu().numpy(), k, True)
+    idx = block.topk_idx.cpu().numpy()
+    sure = route["margin"] >= 1e-4
+    assert np.array_equal(idx[sure], route["idx"][sure])
+    perm, inv = (t.cpu().numpy() for t in (block.perm, block.inv_perm))
+    off, mask = block.offsets.cpu().numpy(), np.ones(E, dtype=bool) if H < 0 else block.hot_mask.cpu().numpy().astype(bool)
+    assert mask.sum() == (E if H < 0 else H)
+    a, h = row_values(block.x8, d), row_values(block.h8, f)
+    y = block.y_perm.cpu().numpy().astype(np.float64)
+    for e in range(E):
+        s = slice(off[e], off[e + 1])
+        if s.start == s.stop:
+            continue
+        if not mask[e]:
+            assert np.isnan(y[s]).all()                     # not written
+            continue
+        v, size = qo.linear(a[perm[s] // k], unpacked(block.w1, e), block.b1[e].cpu().numpy().astype(np.float64), act)
+        err = sum_error(d) * size
+        if act == "gelu":
+            err = 1.13 * err + 1e-6 * np.maximum(1, size)
+        assert_codes(codes_of(block.h8.codes[s]), block.h8.scales[s].cpu().numpy().astype(np.float64), v, err, f)
+        v, size = qo.linear(h[s], unpacked(block.w2, e), block.b2[e].cpu().numpy().astype(np.float64))
+        assert (np.abs(y[s] - v) <= sum_error(f) * size + HALF["f32"] * np.abs(v)).all()
+    gate = block.topk_w.cpu().numpy().astype(np.float64)
+    want, size = np.zeros((T, d)), np.zeros((T, d))
+    for j in range(k):
+        on = mask[idx[:, j]]
+        rows = y[inv.reshape(T, k)[:, j]]
+        want[on] += gate[on, j:j + 1] * rows[on]
+        size[on] += np.abs(gate[on, j:j + 1] * rows[on])
+    got = out.float().cpu().numpy().astype(np.float64)
+    assert (np.abs(got - want) <= HALF["bf16"] * np.abs(want) * 1.001 + 8 * HALF["f32"] * size).all()
+
+
+def test_block_of_another_size_and_refusals(gpu_lib):
+    from paper_2405_18832_amd.quant_layer import QuantMoEBlock, QuantWeights
+    say("[case] QuantMoEBlock resized")
+    gen, new, x, r = block_inputs(200, 128, 5)
+    w1, w2 = (new(8, 256, 128) / 11).bfloat16(), (new(8, 128, 256) / 16).bfloat16()
+    block = QuantMoEBlock(200, 128, 256, 8, 2, w1, w2, new(8, 128).bfloat16())
+    whole = block.forward(x, r)[0].clone()
+    one = block.resized(1)
+    assert one.w1 is block.w1 and one.out.shape == (1, 128)
+    out, _ = one.forward(x[7:8].contiguous(), r[7:8].contiguous())
+    # the gate's sums are taken another way for few tokens: the same experts, weights to fp32
+    assert torch.equal(one.topk_idx[0], block.topk_idx[7])
+    assert (out.float() - whole[7].float()).abs().max() <= 2.0 ** -6 * whole[7].float().abs().max()
+    with pytest.raises(ValueError):
+        QuantWeights(w1, torch.ones((8, 2, 1), device="cuda"))
+    with pytest.raises(ValueError):
+        QuantWeights(w1.to(torch.float8_e4m3fn), torch.ones((8, 1, 1), device="cuda"))
+    with pytest.raises(ValueError):
+        QuantMoEBlock(200, 128, 256, 8, 2, w2, w1, new(8, 128).bfloat16())
+
+
+@pytest.mark.parametrize("T,d,f", [(1, 256, 1024), (40, 130, 300), (600, 256, 512)])
+def test_dense_block(gpu_lib, T, d, f):
+    from paper_2405_18832_amd.quant_layer import QuantDenseBlock
+    say(f"[case] QuantDenseBlock T={T} d={d} f={f}")
+    gen, new, x, r = block_inputs(T, d, T + d)
+    block = QuantDenseBlock(T, d, f, new(f, d) / d ** 0.5, new(d, f) / f ** 0.5, torch.exp(0.2 * new(d)), b1=0.3 * new(f), b2=0.3 * new(d))
+    out, _ = block.forward(x, r)
+    torch.cuda.synchronize()
+    check_norm(block, x, r, d)
+    v, size = qo.linear(row_values(block.x8, d), unpacked(block.w1, 0), block.b1.cpu().numpy().astype(np.float64), "relu")
+    assert_codes(codes_of(block.h8.codes), block.h8.scales.cpu().numpy().astype(np.float64), v, sum_error(d) * size, f)
+    v, size = qo.linear(row_values(block.h8, f), unpacked(block.w2, 0), block.b2.cpu().numpy().astype(np.float64))
+    check_rows(out, None, v, sum_error(f) * size, "bf16")
