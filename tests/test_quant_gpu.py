@@ -239,7 +239,9 @@ def check_rows(got, scales, ref, err, out):
 
 
 LINEAR = [(1, 1, 1), (1, 16, 128), (2, 100, 130), (16, 128, 256), (17, 48, 7), (33, 384, 500), (48, 130, 384), (64, 200, 640), (65, 256, 128),
-          (100, 129, 1000), (128, 256, 256), (200, 512, 2048), (257, 384, 512), (300, 260, 1152), (520, 768, 256), (700, 130, 96), (1000, 520, 768)]
+          (100, 129, 1000), (128, 256, 256), (200, 512, 2048), (257, 384, 512), (300, 260, 1152), (520, 768, 256), (700, 130, 96), (1000, 520, 768),
+          # enough units for tiles of 128 and of 256 rows; contractions shorter than the rings
+          (3000, 1024, 128), (2950, 1000, 200), (5000, 2048, 100), (5001, 2050, 384), (4900, 2048, 640)]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16", "e4m3"])
@@ -272,6 +274,9 @@ GROUPS = {
     "large_and_small": ([300, 3, 0, 260, 70, 1, 130, 512], 2, 384, 512),
     "many": ([1, 0, 2] * 340, 2, 32, 64),
     "long": ([700, 2], 1, 520, 2176),
+    # every kind of tile and streamed experts in one launch, with tiles of 256 and of 128 rows
+    "all_kinds": ([1300, 70, 3, 0, 256, 190, 2000, 64, 1000, 257, 17, 65], 2, 2048, 300),
+    "all_kinds_128": ([1300, 70, 3, 0, 256, 190, 64, 900, 257, 17, 65], 2, 1000, 200),
 }
 
 
