@@ -197,12 +197,49 @@ __device__ __forceinline__ void finish_values(const QuantArgs& a, int e, int n0,
     activate_values(a.act, acc);
 }
 
+// Lane group g (of 16) holds v[nf] = columns 16 nf + 4 g ...; afterwards v[i] = columns 16 g + 4 i ...: a lane's four pieces are
+// neighbours, so that it stores 16 bytes instead of four times 4 (a store of 4 bytes per lane to 16 rows costs the memory path as much
+// as one of 16).
+__device__ __forceinline__ void gather_columns(uint32_t (&v)[4]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const auto s = __builtin_amdgcn_permlane32_swap(v[i], v[i + 2], false, false);
+        v[i] = s[0];
+        v[i + 2] = s[1];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+        const auto s = __builtin_amdgcn_permlane16_swap(v[i], v[i + 1], false, false);
+        v[i] = s[0];
+        v[i + 1] = s[1];
+    }
+}
+
 template <int OUT, int STRIDE, int NF, int TF>
 __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row0, int rows, const f32x4 (&acc)[NF][TF]) {
     static_assert(OUT != kOutE4m3, "");
     const int lane = here(threadIdx.x) & 63, r = lane & 15, g = lane >> 4;
     // four columns at once where every row begins on a boundary of four
     const bool wide = a.N % 4 == 0 && reinterpret_cast<uintptr_t>(a.out) % (OUT == kOutF32 ? 16 : 8) == 0;
+    if (OUT == kOutBf16 && NF == 4 && a.N % 8 == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0) {
+#pragma unroll
+        for (int tf = 0; tf < TF; ++tf) {
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int nf = 0; nf < 4; ++nf) {
+                lo[nf] = pack_bf16x2(acc[nf % NF][tf][0], acc[nf % NF][tf][1]);
+                hi[nf] = pack_bf16x2(acc[nf % NF][tf][2], acc[nf % NF][tf][3]);
+            }
+            gather_columns(lo);
+            gather_columns(hi);
+            if (tf * STRIDE + r >= rows) continue;
+            const int n = n0 + g * 16;
+            uint16_t* out = static_cast<uint16_t*>(a.out) + static_cast<size_t>(row0 + tf * STRIDE + r) * a.N + n;
+            if (n < a.N) *reinterpret_cast<uint4*>(out) = uint4{lo[0], hi[0], lo[1], hi[1]};
+            if (n + 8 < a.N) *reinterpret_cast<uint4*>(out + 8) = uint4{lo[2], hi[2], lo[3], hi[3]};
+        }
+        return;
+    }
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
         if (tf * STRIDE + r >= rows) continue;
@@ -255,17 +292,24 @@ __device__ __forceinline__ void store_codes(const QuantArgs& a, int n0, int row0
     const size_t pitch = quant_pitch(a.N);
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
-        if (tf * STRIDE + r >= rows) continue;
         const size_t row = static_cast<size_t>(row0 + tf * STRIDE + r);
         const float scale = block_scale(most[tf]), inv = __builtin_amdgcn_rcpf(scale);
-        uint8_t* out = static_cast<uint8_t*>(a.out) + row * pitch;
+        uint32_t codes[NF];
 #pragma unroll
         for (int nf = 0; nf < NF; ++nf) {
             const int n = n0 + nf * 16 + g * 4;
             const f32x4 v = acc[nf][tf];
-            uint32_t codes = pack_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
-            if (n + 4 > a.N) codes = n >= a.N ? 0u : codes & (0xffffffffu >> (8 * (n + 4 - a.N)));     // zeros past the end
-            *reinterpret_cast<uint32_t*>(out + n) = codes;
+            codes[nf] = pack_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            if (n + 4 > a.N) codes[nf] = n >= a.N ? 0u : codes[nf] & (0xffffffffu >> (8 * (n + 4 - a.N)));     // zeros past the end
+        }
+        if constexpr (NF == 4) gather_columns(codes);
+        if (tf * STRIDE + r >= rows) continue;
+        uint8_t* out = static_cast<uint8_t*>(a.out) + row * pitch + n0;
+        if constexpr (NF == 4) {
+            *reinterpret_cast<uint4*>(out + g * 16) = uint4{codes[0], codes[1], codes[2], codes[3]};
+        } else {
+#pragma unroll
+            for (int nf = 0; nf < NF; ++nf) *reinterpret_cast<uint32_t*>(out + nf * 16 + g * 4) = codes[nf];
         }
         if (scales && g == 0) a.out_scales[row * quant_blocks(a.N) + n0 / kQuantBlock] = scale;
     }
