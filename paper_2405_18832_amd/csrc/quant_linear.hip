@@ -351,16 +351,22 @@ __device__ __forceinline__ int row_operand(int tid, int first) {
 __device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 : 64; }
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
-// Unit: an expert's rows, at most 64, x 128 columns, by 8 wavefronts of 16 columns each, a block of 128 columns of the contraction per
-// step.  Bound by memory, so what matters is that copies never stop: weights (16 KiB a step), rows and scales go to LDS directly, through
-// a ring of six stages that runs on across units.  A block's units follow each other in one expert, where nothing needs to be looked up
-// (a load that the compiler sees would make it wait for every copy in flight).
-constexpr int kStreamRows = 64, kStreamWaves = 8, kStreamStages = 6, kStreamCopies = 4;
-constexpr int kStreamX = kQuantBlock * kQuantBlock, kStreamS = kStreamX + kStreamRows * kQuantBlock;
-constexpr int kStreamStage = kStreamS + 4 * 256;            // scales of the rows, of the weights (64 times), bias of the 128 columns
-constexpr int kStreamMost = kStreamStages * kStreamStage, kStreamList = kStreamMost + kStreamWaves * kStreamRows * 4;
-constexpr int kStreamLdsBytes = kStreamList + MOE_MAX_E * 2 + kStreamWaves * 4;
-static_assert(kStreamLdsBytes <= 160 * 1024, "fits a CU");
+// Unit: an expert's rows, at most 64, x 128 NF columns, by 8 wavefronts of 16 NF columns each, a block of 128 columns of the contraction
+// per step.  Bound by memory, so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
+// through a ring of stages that runs on across units.  A block's units follow each other in one expert, where nothing needs to be looked
+// up (a load that the compiler sees would make it wait for every copy in flight).
+constexpr int kStreamRows = 64, kStreamWaves = 8;
+template <int NF>
+struct Streams {
+    static constexpr int kStages = NF == 1 ? 6 : 3, kCols = NF * kQuantBlock;
+    static constexpr int kX = kCols * kQuantBlock, kS = kX + kStreamRows * kQuantBlock;
+    // pieces of 256 bytes: scales of the rows, scale of each 128 columns (64 times), bias of the columns
+    static constexpr int kPieces = 1 + 3 * NF, kSw = kS + 256, kBias = kSw + NF * 256, kStage = kS + kPieces * 256;
+    static constexpr int kMost = kStages * kStage, kList = kMost + kStreamWaves * kStreamRows * 4;
+    static constexpr int kLdsBytes = kList + MOE_MAX_E * 2 + kStreamWaves * 4;
+    static constexpr int kCopies = 2 * NF + 2;          // a wavefront's, per stage
+    static_assert(kLdsBytes <= 160 * 1024 && kPieces <= kStreamWaves, "fits a CU");
+};
 
 // The experts of 1 ... max_rows rows, in order, counted by every block for itself; returns how many.  `tmp`: an int per wavefront.
 template <int THREADS>
@@ -389,14 +395,15 @@ __device__ __forceinline__ int list_experts(const QuantArgs& a, int max_rows, ui
 // OUT = kOutParts: the contraction is cut into `split` parts, whose sums go to a.out as [split][rows][pitch of N] fp32.
 constexpr int kOutParts = 3;
 
-template <int OUT>
-__device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, int parts_wanted, int b, unsigned char* smem) {
+template <int OUT, int NF>
+__device__ __forceinline__ void stream_units(const QuantArgs& a, int tiles, int parts_wanted, int b, unsigned char* smem) {
+    using S = Streams<NF>;
+    constexpr int kStages = S::kStages, kStage = S::kStage;
     const int split = OUT == kOutParts ? parts_wanted : 1;
-    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + kStreamMost);         // [64][8]
-    uint16_t* list = reinterpret_cast<uint16_t*>(smem + kStreamList);
-    const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
+    uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + S::kMost);         // [64][8]
+    const uint16_t* list = reinterpret_cast<const uint16_t*>(smem + Streams<1>::kList);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
-    const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
+    const int KB = quant_blocks(a.K), blocks = quant_blocks(a.N), groups = (blocks + NF - 1) / NF;
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
     const int per_tile = groups * split, units = tiles * per_tile;
 
@@ -436,9 +443,10 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
         return w;
     };
 
-    // copies: wavefront w brings rows 8 w ... 8 w + 7, weight fragment w, and a quarter of the scales and bias (two wavefronts each)
+    // copies: wavefront w brings rows 8 w ... 8 w + 7, weight fragments NF w ..., and one of the pieces of scales and bias (some twice)
     const uint32_t lds = lds_address(smem);
-    const uint32_t to_weights = lds + wave * kFragBytes, to_rows = lds + kStreamX + wave * 1024, to_scales = lds + kStreamS + (wave & 3) * 256;
+    const int piece = NF == 1 ? wave & 3 : min(wave, S::kPieces - 1);
+    const uint32_t to_weights = lds + wave * NF * kFragBytes, to_rows = lds + S::kX + wave * 1024, to_scales = lds + S::kS + piece * 256;
     const uint8_t *tile_row, *row_from, *weights_from;
     const float *tile_scale, *scales_from;
     int scales_step;
@@ -449,21 +457,25 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
     };
     auto point_at = [&](const Unit& w) __attribute__((always_inline)) {
         row_from = tile_row + static_cast<size_t>(w.kb) * kQuantBlock;
-        weights_from = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) +
-                       (static_cast<size_t>(w.group * 8 + wave) * KB + w.kb) * kFragBytes + lane * 16;
-        const int quarter = wave & 3;
+        // columns of the last unit that do not exist are read as the last ones that do, and not stored
+        const int fragment = min(w.group * 8 * NF + wave * NF, blocks * 8 - NF);
+        weights_from = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) + (static_cast<size_t>(fragment) * KB + w.kb) * kFragBytes + lane * 16;
         scales_step = 1;
-        if (quarter == 0) scales_from = tile_scale + w.kb;
-        else if (quarter == 1 || a.bias == nullptr) scales_from = a.w_scales + (static_cast<size_t>(w.e) * groups + w.group) * KB + w.kb;
+        if (piece == 0) scales_from = tile_scale + w.kb;
+        else if (piece <= NF || a.bias == nullptr) scales_from = a.w_scales + (static_cast<size_t>(w.e) * blocks + min(w.group * NF + min(piece, NF) - 1, blocks - 1)) * KB + w.kb;
         else {
-            scales_from = a.bias + static_cast<size_t>(w.e) * a.N + min(w.group * kQuantBlock + (quarter - 2) * 64 + lane, a.N - 1);
+            scales_from = a.bias + static_cast<size_t>(w.e) * a.N + min(w.group * S::kCols + (piece - 1 - NF) * 64 + lane, a.N - 1);
             scales_step = 0;
         }
     };
     auto stage_in = [&](int slot) {
-        const int at = slot * kStreamStage;
-        copy16_to_lds(weights_from, to_weights + at);
-        copy16_to_lds(weights_from + 1024, to_weights + at + 1024);
+        const int at = slot * kStage;
+#pragma unroll
+        for (int nf = 0; nf < NF; ++nf) {
+            const uint8_t* from = weights_from + static_cast<size_t>(nf) * KB * kFragBytes;
+            copy16_to_lds(from, to_weights + at + nf * kFragBytes);
+            copy16_to_lds(from + 1024, to_weights + at + nf * kFragBytes + 1024);
+        }
         copy16_to_lds(row_from, to_rows + at);
         copy4_to_lds(scales_from, to_scales + at);
         weights_from += kFragBytes;
@@ -484,9 +496,9 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
         } else {
             // nothing left to copy: copies of some scale to the slot that has fallen free keep up the count that the waits go by
 #pragma unroll
-            for (int i = 0; i < kStreamCopies; ++i) copy4_to_lds(tile_scale, to_scales + slot_in * kStreamStage);
+            for (int i = 0; i < S::kCopies; ++i) copy4_to_lds(tile_scale, to_scales + slot_in * kStage);
         }
-        slot_in = slot_in == kStreamStages - 1 ? 0 : slot_in + 1;
+        slot_in = slot_in == kStages - 1 ? 0 : slot_in + 1;
         ++ahead.kb;
         if (ahead.kb == ahead.kb1) {
             if (--units_in > 0) {
@@ -503,52 +515,66 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
         }
     };
 #pragma unroll 1
-    for (int i = 0; i < kStreamStages - 1; ++i) copy_next();
+    for (int i = 0; i < kStages - 1; ++i) copy_next();
 
     Unit cur = unit_at(tile0, first - tile0 * per_tile);
-    const int at_w = wave * kFragBytes + lane * 16, at_x = kStreamX + row_operand(threadIdx.x, 0), x_other = row_operand_other(at_x);
-    const int at_sx = kStreamS + r * 4, at_sw = kStreamS + 256, at_bias = kStreamS + 512 + (wave * 16 + (lane >> 4) * 4) * 4;
+    const int at_w = wave * NF * kFragBytes + lane * 16, at_x = S::kX + row_operand(threadIdx.x, 0), x_other = row_operand_other(at_x);
+    const int at_sx = S::kS + r * 4, at_sw = S::kSw + wave * NF / 8 * 256, at_bias = S::kBias + (wave * NF * 16 + (lane >> 4) * 4) * 4;
     int slot = 0;
     while (true) {
         auto run_unit = [&](auto tf_const) __attribute__((always_inline)) {
             constexpr int TF = decltype(tf_const)::value;
-            f32x4 acc[1][TF];
+            f32x4 acc[NF][TF], bias[NF];
 #pragma unroll
-            for (int tf = 0; tf < TF; ++tf) acc[0][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
-            f32x4 bias = {0.f, 0.f, 0.f, 0.f};
+            for (int nf = 0; nf < NF; ++nf)
+#pragma unroll
+                for (int tf = 0; tf < TF; ++tf) acc[nf][tf] = f32x4{0.f, 0.f, 0.f, 0.f};
             for (; cur.kb < cur.kb1; ++cur.kb) {
-                copies_landed<(kStreamStages - 2) * kStreamCopies>();
-                const unsigned char* st = smem + slot * kStreamStage;
-                const i32x8 w = read_codes(st + at_w, 1024);
-                const float sw = *reinterpret_cast<const float*>(st + at_sw);
-                i32x8 x[TF];
+                copies_landed<(kStages - 2) * S::kCopies>();
+                const unsigned char* st = smem + slot * kStage;
+                i32x8 w[NF], x[TF];
                 float sx[TF];
+#pragma unroll
+                for (int nf = 0; nf < NF; ++nf) w[nf] = read_codes(st + at_w + nf * kFragBytes, 1024);
+                const float sw = *reinterpret_cast<const float*>(st + at_sw);
 #pragma unroll
                 for (int tf = 0; tf < TF; ++tf) x[tf] = read_codes(st + at_x + tf * kFragBytes, x_other);
 #pragma unroll
                 for (int tf = 0; tf < TF; ++tf) sx[tf] = *reinterpret_cast<const float*>(st + at_sx + tf * 64);
-                if constexpr (OUT != kOutParts) bias = *reinterpret_cast<const f32x4*>(st + at_bias);
+                if constexpr (OUT != kOutParts) {
+#pragma unroll
+                    for (int nf = 0; nf < NF; ++nf) bias[nf] = *reinterpret_cast<const f32x4*>(st + at_bias + nf * 64);
+                }
                 copy_next();
-                // a quarter of the block after the other, so that the row fragments' sums are independent of each other and codes are
+                // a quarter of the block after the other, so that the fragments' sums are independent of each other and codes are
                 // widened while others are multiplied
-                f32x4 p[TF];
+                f32x4 p[NF][TF];
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const bf16x8 wide = widen8(w, k);
+                    bf16x8 wide[NF];
 #pragma unroll
-                    for (int tf = 0; tf < TF; ++tf)
-                        p[tf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide, widen8(x[tf], k), k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p[tf], 0, 0, 0);
+                    for (int nf = 0; nf < NF; ++nf) wide[nf] = widen8(w[nf], k);
+#pragma unroll
+                    for (int tf = 0; tf < TF; ++tf) {
+                        const bf16x8 row = widen8(x[tf], k);
+#pragma unroll
+                        for (int nf = 0; nf < NF; ++nf)
+                            p[nf][tf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[nf], row, k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p[nf][tf], 0, 0, 0);
+                    }
                 }
 #pragma unroll
                 for (int tf = 0; tf < TF; ++tf) {
                     const float scale = sx[tf] * sw;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[0][tf][i] = fmaf(scale, p[tf][i], acc[0][tf][i]);
+                    for (int nf = 0; nf < NF; ++nf)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[nf][tf][i] = fmaf(scale, p[nf][tf][i], acc[nf][tf][i]);
                 }
-                slot = slot == kStreamStages - 1 ? 0 : slot + 1;
+                slot = slot == kStages - 1 ? 0 : slot + 1;
             }
-            const int n0 = cur.group * kQuantBlock + wave * 16;
+            const int n0 = cur.group * S::kCols + wave * NF * 16;
             if constexpr (OUT == kOutParts) {
+                static_assert(NF == 1, "calls of few rows are cut, which have few columns per unit");
                 float* parts = static_cast<float*>(a.out) + static_cast<size_t>(cur.part) * a.rows * quant_pitch(a.N);
 #pragma unroll
                 for (int tf = 0; tf < TF; ++tf)
@@ -558,10 +584,13 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
             } else {
                 if (a.bias != nullptr) {
 #pragma unroll
-                    for (int tf = 0; tf < TF; ++tf) acc[0][tf] += bias;
+                    for (int nf = 0; nf < NF; ++nf)
+#pragma unroll
+                        for (int tf = 0; tf < TF; ++tf) acc[nf][tf] += bias[nf];
                 }
                 activate_values(a.act, acc);
                 if constexpr (OUT == kOutE4m3) {
+                    constexpr int kSharing = kStreamWaves / NF;         // wavefronts whose columns share a scale
                     uint32_t most[TF];
                     row_magnitudes(a.N, n0, acc, most);
                     if (lane < 16) {
@@ -572,11 +601,11 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
 #pragma unroll
                     for (int tf = 0; tf < TF; ++tf)
 #pragma unroll
-                        for (int v = 0; v < kStreamWaves; v += 4) {
-                            const uint4 m = *reinterpret_cast<const uint4*>(mosts + (tf * 16 + r) * kStreamWaves + v);
+                        for (int v = 0; v < kSharing; v += 4) {
+                            const uint4 m = *reinterpret_cast<const uint4*>(mosts + (tf * 16 + r) * kStreamWaves + wave / kSharing * kSharing + v);
                             most[tf] = max(most[tf], max(max(m.x, m.y), max(m.z, m.w)));
                         }
-                    store_codes<16>(a, n0, cur.row0, cur.rows, acc, most, wave == 0);
+                    if (n0 < blocks * kQuantBlock) store_codes<16>(a, n0, cur.row0, cur.rows, acc, most, wave % kSharing == 0);
                 } else {
                     store_values<OUT, 16>(a, n0, cur.row0, cur.rows, acc);
                 }
@@ -596,7 +625,9 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int max_rows, i
 template <int OUT>
 __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
     extern __shared__ __align__(16) unsigned char smem[];
-    stream_units<OUT>(a, max_rows, parts_wanted, blockIdx.x, smem);
+    uint16_t* list = reinterpret_cast<uint16_t*>(smem + Streams<1>::kList);
+    const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
+    stream_units<OUT, 1>(a, tiles, parts_wanted, blockIdx.x, smem);
 }
 
 // Adds up the parts of a split contraction, in their order, and finishes the rows.  A block of threads per row and 8 groups of 128
@@ -968,7 +999,14 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_product_kernel(const Qu
     tile_units<OUT, RMAX>(a, tiled_min_rows, smem);
     if (a.offsets == nullptr) return;
     __syncthreads();
-    stream_units<OUT>(a, tiled_min_rows - 1, 1, gridDim.x - 1 - blockIdx.x, smem);
+    static_assert(Streams<1>::kList >= Streams<2>::kList, "the list lies behind both rings");
+    uint16_t* list = reinterpret_cast<uint16_t*>(smem + Streams<1>::kList);
+    const int tiles = list_experts<kTileWaves * 64>(a, tiled_min_rows - 1, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
+    const int b = gridDim.x - 1 - blockIdx.x;
+    // Units of 256 columns widen each row fragment for twice the columns; but where those of 128 are at most one per block they use
+    // more of the CUs.
+    if (tiles * quant_blocks(a.N) > static_cast<int>(gridDim.x)) stream_units<OUT, 2>(a, tiles, 1, b, smem);
+    else stream_units<OUT, 1>(a, tiles, 1, b, smem);
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
@@ -1007,7 +1045,7 @@ static int tile_fragments(int rows, int N, size_t operand_bytes) {
 
 // dynamic LDS of the kernel with both kinds of units
 template <int RMAX>
-constexpr int kProductLds = Tiles<RMAX>::kLdsBytes > kStreamLdsBytes ? Tiles<RMAX>::kLdsBytes : kStreamLdsBytes;
+constexpr int kProductLds = Tiles<RMAX>::kLdsBytes > Streams<1>::kLdsBytes ? Tiles<RMAX>::kLdsBytes : Streams<1>::kLdsBytes;
 
 template <int OUT, int RMAX>
 static void launch_tiles(const QuantArgs& a, int grid, hipStream_t stream) {
@@ -1022,7 +1060,7 @@ static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
     if (split > 1) {
         QuantArgs parts = a;
         parts.out = ws;
-        quant_stream_kernel<kOutParts><<<grid, threads, kStreamLdsBytes, stream>>>(parts, a.rows, split);
+        quant_stream_kernel<kOutParts><<<grid, threads, Streams<1>::kLdsBytes, stream>>>(parts, a.rows, split);
         quant_join_kernel<OUT><<<dim3(a.rows, (quant_blocks(a.N) + 7) / 8), dim3(256), 0, stream>>>(a, static_cast<const float*>(ws), split);
         return hipGetLastError();
     }
@@ -1032,7 +1070,7 @@ static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
         else if (r == 2) launch_tiles<OUT, 2>(a, cus, stream);
         else launch_tiles<OUT, 1>(a, cus, stream);
     } else {
-        quant_stream_kernel<OUT><<<grid, threads, kStreamLdsBytes, stream>>>(a, a.rows, 1);
+        quant_stream_kernel<OUT><<<grid, threads, Streams<1>::kLdsBytes, stream>>>(a, a.rows, 1);
     }
     return hipGetLastError();
 }
@@ -1050,10 +1088,10 @@ hipError_t configure_quant_kernels() {
                {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 4>), kProductLds<4>},
                {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 2>), kProductLds<2>},
                {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 1>), kProductLds<1>},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutF32>), kStreamLdsBytes},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutBf16>), kStreamLdsBytes},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutE4m3>), kStreamLdsBytes},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutParts>), kStreamLdsBytes}};
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutF32>), Streams<1>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutBf16>), Streams<1>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutE4m3>), Streams<1>::kLdsBytes},
+               {reinterpret_cast<const void*>(quant_stream_kernel<kOutParts>), Streams<1>::kLdsBytes}};
     for (const auto& k : all) {
         const hipError_t e = hipFuncSetAttribute(k.kernel, hipFuncAttributeMaxDynamicSharedMemorySize, k.lds);
         if (e != hipSuccess) return e;
