@@ -380,8 +380,10 @@ size_t moe_quant_workspace_bytes(const moe_quant_shape* shape);
 
 /*
  * out[r, n] = act( sum_b sa[r, b] * sw[n/128, b] * sum_{c in block b} a[r, c] * w[n, c] + bias[n] )
- * a, sa: quantised rows [rows, K]; w, sw: packed weights and their scales (E = 1); bias [N] fp32 or NULL.  Code products and sums are
- * accumulated in fp32 and the result is rounded once, to out_dtype.  out_scales: scales of the quantised output, NULL for the
+ * a, sa: quantised rows [rows, K]; w, sw: packed weights and their scales (E = 1); bias [N] fp32 or NULL.  The blocks' sums are added up in
+ * fp32 and the result is rounded once, to out_dtype.  For an out_dtype of MOE_F32 the sums within a block are fp32 as well; for the others they
+ * may come from the matrix units for 8-bit operands, which cut products at 2^-13 of the largest of each eight (1.5e-5 of the rms of a sum
+ * of normal values).  out_scales: scales of the quantised output, NULL for the
  * other types.  ws: at least moe_quant_workspace_bytes, 256-byte aligned.  Outputs overlap nothing.
  */
 moe_status moe_quant_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const void* w, const float* w_scales,

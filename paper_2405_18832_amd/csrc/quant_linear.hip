@@ -40,9 +40,19 @@ __device__ __forceinline__ Widened widen(const i32x8& codes) {
 
 // The matrix instruction's first operand is 16 weight rows, the second one 16 token rows.  Lane l holds 32 codes of row l % 16 of each;
 // which columns they are does not matter as long as both operands agree (moe.h: 64 h + 16 (l / 16), h = 0, 1).  Result i of lane l: weight
-// row 4 (l / 16) + i, token row l % 16.  The bf16 units are used: those for 8-bit operands (v_mfma_f32_16x16x128_f8f6f4) add up groups of
-// products after aligning them to the largest and drop what lies below about 2^-14 of it, which is 1.5e-5 of the rms of a sum of 128
-// products of normal values.
+// row 4 (l / 16) + i, token row l % 16.
+//
+// Which matrix units: those for 8-bit operands (v_mfma_f32_16x16x128_f8f6f4) take twice the products per cycle and need no widened codes,
+// but add products in groups of eight neighbours, cut at 2^-13 of the power of two of the group's largest; the groups' sums are fp32.
+// Measured: 1.5e-5 of the rms of a sum of 128 products of normal values, 5e-5 where one column of a block is 50 times the others, which is a
+// hundredth of half a step of bf16 and less than a thousandth of one of e4m3.  So outputs of these types use them, and every block's sum is
+// added to the others in fp32: 16384 x 8192 x 2048 (GeLU, e4m3) 556 -> 400 us, 1501 x 768 x 3072 (bf16) 24.4 -> 14.6.  fp32 outputs, and the
+// parts of a cut contraction, which are fp32, use the bf16 units, whose sums of widened codes are exact to 1e-8 of the rms.
+template <int OUT> constexpr bool kEightBitUnits = OUT == kOutBf16 || OUT == kOutE4m3;
+__device__ __forceinline__ f32x4 multiply_codes(const i32x8& w, const i32x8& x) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);     // e4m3 both, scales of one
+}
+
 __device__ __forceinline__ float quant_activate(float v, int act) {
     if (act == MOE_ACT_GELU) return gelu_exp(v);
     if (act == MOE_ACT_RELU) return v < 0.f ? 0.f : v;      // NaN stays
@@ -546,20 +556,27 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int tiles, int 
                     for (int nf = 0; nf < NF; ++nf) bias[nf] = *reinterpret_cast<const f32x4*>(st + at_bias + nf * 64);
                 }
                 copy_next();
-                // a quarter of the block after the other, so that the fragments' sums are independent of each other and codes are
-                // widened while others are multiplied
                 f32x4 p[NF][TF];
+                if constexpr (kEightBitUnits<OUT>) {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    bf16x8 wide[NF];
+                    for (int tf = 0; tf < TF; ++tf)
 #pragma unroll
-                    for (int nf = 0; nf < NF; ++nf) wide[nf] = widen8(w[nf], k);
+                        for (int nf = 0; nf < NF; ++nf) p[nf][tf] = multiply_codes(w[nf], x[tf]);
+                } else {
+                    // a quarter of the block after the other, so that the fragments' sums are independent of each other and codes are
+                    // widened while others are multiplied
 #pragma unroll
-                    for (int tf = 0; tf < TF; ++tf) {
-                        const bf16x8 row = widen8(x[tf], k);
+                    for (int k = 0; k < 4; ++k) {
+                        bf16x8 wide[NF];
 #pragma unroll
-                        for (int nf = 0; nf < NF; ++nf)
-                            p[nf][tf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[nf], row, k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p[nf][tf], 0, 0, 0);
+                        for (int nf = 0; nf < NF; ++nf) wide[nf] = widen8(w[nf], k);
+#pragma unroll
+                        for (int tf = 0; tf < TF; ++tf) {
+                            const bf16x8 row = widen8(x[tf], k);
+#pragma unroll
+                            for (int nf = 0; nf < NF; ++nf)
+                                p[nf][tf] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide[nf], row, k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p[nf][tf], 0, 0, 0);
+                        }
                     }
                 }
 #pragma unroll
@@ -708,6 +725,7 @@ struct Tiles {
 template <int OUT, int RMAX>
 __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, unsigned char* smem) {
     using T = Tiles<RMAX>;
+    constexpr bool EIGHT = kEightBitUnits<OUT>;
     constexpr int kStages = T::kStages, kStageW = T::kStageW, kStageS = T::kStageS, kStage = T::kStage, tile_rows = T::kRows;
     uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + T::kMost);           // [2][rows]
     int4* counts = reinterpret_cast<int4*>(smem + T::kStarts);
@@ -838,10 +856,16 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
         if (++kb_in == KB) next_unit();
     };
     Unit cur = ahead;
-    copy_next();
-    copies_landed<0>();
+    if constexpr (EIGHT) {
 #pragma unroll 1
-    for (int i = 0; i < kStages - 2; ++i) copy_next();
+        for (int i = 0; i < kStages; ++i) copy_next();
+        copies_landed<(kStages - 1) * T::kCopies>();
+    } else {
+        copy_next();
+        copies_landed<0>();
+#pragma unroll 1
+        for (int i = 0; i < kStages - 2; ++i) copy_next();
+    }
 
     int slot = 0;
     auto run_unit = [&](auto fragments) __attribute__((always_inline)) {
@@ -859,109 +883,173 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
         for (int nf = 0; nf < 4; ++nf)
 #pragma unroll
             for (int i = 0; i < R; ++i) acc[nf][i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        // A step is 2 R rounds of eight matrix instructions, two weight fragments x one row fragment.  What the vector unit has to do
-        // is spread between them, one piece after each: the codes of the next row fragment are widened, the sums of the round before
-        // are added to the accumulators; in the last round and in the next step's first one also the next stage's weights are widened,
-        // two fragments each, as their registers fall free.  The order is held by the scheduling barriers.
-        // At the beginning of a step: w[0], w[1] and the first row fragment widened, the codes of w[2], w[3] and half of the
-        // second row fragment's (if there is one), and the sums of the last round before it.
-        Widened w[4], x[2];
-        i32x8 codes_w[2], next_w[2];
-        i32x4 codes_x[2];                   // halves of the fragment that is widened next
-        f32x4 sums[2][2] = {};
-        float last_scale = 0.f;
-        const unsigned char* st0 = smem + slot * kStage;
-        w[0] = widen(weight_codes(st0, 0));
-        w[1] = widen(weight_codes(st0, 1));
-        codes_w[0] = weight_codes(st0, 2);
-        codes_w[1] = weight_codes(st0, 3);
-        x[0] = widen(row_codes(st0, 0));
-        codes_x[0] = row_codes_half(st0, 1, 0);
         // the steps to the end of the unit or to where the copies go on to the next one: without a branch, so that the order stays
+        auto all_steps = [&](auto step) __attribute__((always_inline)) {
 #pragma unroll 1
-        for (int j = 0; j < KB;) {
-        // behind branches that not every lane takes, such as the stores of the unit before
-        u_in = uniform(u_in);
-        kb_in = uniform(kb_in);
-        slot_in = uniform(slot_in);
-        slot = uniform(slot);
-        stage_step = uniform(stage_step);
-        weights_base = uniform(weights_base);
-        if constexpr (OFFSETS) {
-            rows_base = uniform(rows_base);
-            scales_base = uniform(scales_base);
-        }
-        const int steps = min(KB - j, KB - kb_in);
-        j += steps;
-        kb_in += steps;
+            for (int j = 0; j < KB;) {
+                // behind branches that not every lane takes, such as the stores of the unit before
+                u_in = uniform(u_in);
+                kb_in = uniform(kb_in);
+                slot_in = uniform(slot_in);
+                slot = uniform(slot);
+                stage_step = uniform(stage_step);
+                weights_base = uniform(weights_base);
+                if constexpr (OFFSETS) {
+                    rows_base = uniform(rows_base);
+                    scales_base = uniform(scales_base);
+                }
+                const int steps = min(KB - j, KB - kb_in);
+                j += steps;
+                kb_in += steps;
 #pragma unroll 1
-        for (int s = 0; s < steps; ++s) {
-            const unsigned char* st = smem + slot * kStage;
-            slot = slot == kStages - 1 ? 0 : slot + 1;
-            const unsigned char* st_next = smem + slot * kStage;
-            float scale[R];
-            const float sw = *reinterpret_cast<const float*>(st + at_sw);
-#pragma unroll
-            for (int i = 0; i < R; ++i) scale[i] = *reinterpret_cast<const float*>(st + at_sx + i * 256);
-#pragma unroll
-            for (int round = 0; round < 2 * R; ++round) {
-                const int i = round >> 1, half = round & 1;
-                if (round == (R > 2 ? 2 * R - 4 : 0)) {     // the next stage has landed, the one after it goes out
-                    __builtin_amdgcn_sched_barrier(0);
-                    copies_landed<(kStages - 3) * T::kCopies>();
-                    if (R == 1) codes_x[0] = row_codes_half(st_next, 0, 0);
+                for (int s = 0; s < steps; ++s) {
+                    step();
+                    next_stage();
                 }
-                // A round ahead of its use: the second half of the fragment that is widened now, the first half of the one after it.
-                // Behind the last row fragment comes the next stage's first.
-                if (half == 0) codes_x[1] = i + 1 < R ? row_codes_half(st, i + 1, 1) : row_codes_half(st_next, 0, 1);
-                else if (R > 1) codes_x[0] = i + 2 < R ? row_codes_half(st, i + 2, 0) : row_codes_half(st_next, i + 2 - R, 0);
-                if (half == 0 && i == R - 1) {
-                    next_w[0] = weight_codes(st_next, 0);
-                    next_w[1] = weight_codes(st_next, 1);
-                }
-                if (R == 1 && round == 1) {                 // one row fragment: their last use was a round ago
-                    w[2] = widen(codes_w[0]);
-                    w[3] = widen(codes_w[1]);
-                }
-                Widened& x_now = x[R > 1 ? i & 1 : 0];
-                Widened& x_later = x[R > 1 ? (i & 1) ^ 1 : 1];
-                const int before = round == 0 ? 2 * R - 1 : round - 1;      // the round whose sums are added
-                const float by = round == 0 ? last_scale : scale[before >> 1] * sw;
-#pragma unroll
-                for (int m = 0; m < 8; ++m) {
-                    const int k = m >> 1, q = m & 1;
-                    f32x4& p = sums[round & 1][q];
-                    p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2 * half + q].eight(k), x_now.eight(k),
-                                                                k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p, 0, 0, 0);
-                    // one copy at a time: issued together they would hold up every wavefront
-                    constexpr int kFirst = R > 2 ? 8 * (2 * R - 4) : 0, kEvery = R == 1 ? 2 : 4;
-                    const int at = 8 * round + m - kFirst;
-                    if (at >= 0 && at % kEvery == 0) copy_piece(at / kEvery);
-                    x_later.widen_two(codes_x[half][m >> 1], half * 8 + m);
-                    f32x4& sum = acc[2 * (before & 1) + (m >> 2)][before >> 1];
-                    sum[m & 3] = fmaf(by, sums[(round & 1) ^ 1][m >> 2][m & 3], sum[m & 3]);
-                    if (R > 1 && round == 0) {
-#pragma unroll
-                        for (int c = 4 * m; c < 4 * m + 4; ++c) w[2 + (c >> 4)].widen_two(codes_w[c >> 4][(c & 15) >> 1], c & 15);
-                    }
-                    if (round == 2 * R - 1) {
-#pragma unroll
-                        for (int c = 4 * m; c < 4 * m + 4; ++c) w[c >> 4].widen_two(next_w[c >> 4][(c & 15) >> 1], c & 15);
-                        if (m == 4) codes_w[0] = weight_codes(st_next, 2);
-                        if (m == 7) codes_w[1] = weight_codes(st_next, 3);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
+                if (kb_in == KB) next_unit();
             }
-            next_stage();
-            last_scale = scale[R - 1] * sw;
-            if (R == 1) x[0] = x[1];
-        }
-        if (kb_in == KB) next_unit();
-        }
+        };
+        if constexpr (EIGHT) {
+            // A step is 4 R matrix instructions: the first two weight fragments x every row fragment, then the other two.  Operands are
+            // read from the next stage into the registers of those that were used last, at least 2 R + 1 instructions (2 of one row
+            // fragment) before their use; a stage's slot is free again in the middle of its own step, so that a copy has two steps to
+            // land in.  A sum is added to its accumulator two instructions after its own.  The order is held by the scheduling barriers.
+            i32x8 w[4], x[R];
+            f32x4 sums[4] = {};
+            float by[R], last = 0.f;
+            const unsigned char* st0 = smem + slot * kStage;
 #pragma unroll
-        for (int m = 0; m < 8; ++m)
-            acc[2 + (m >> 2)][R - 1][m & 3] = fmaf(last_scale, sums[1][m >> 2][m & 3], acc[2 + (m >> 2)][R - 1][m & 3]);
+            for (int nf = 0; nf < 4; ++nf) w[nf] = weight_codes(st0, nf);
+#pragma unroll
+            for (int i = 0; i < R; ++i) x[i] = row_codes(st0, i);
+#pragma unroll
+            for (int i = 0; i < R; ++i) by[i] = *reinterpret_cast<const float*>(st0 + at_sx + i * 256) * *reinterpret_cast<const float*>(st0 + at_sw);
+            all_steps([&]() __attribute__((always_inline)) {
+                constexpr int M = 4 * R, kFirst = R == 1 ? 0 : M / 2;       // from where on the next stage is read and copies go out
+                slot = slot == kStages - 1 ? 0 : slot + 1;
+                const unsigned char* st = smem + slot * kStage;
+                float next_sx[R], next_sw = 0.f;
+#pragma unroll
+                for (int n = 0; n < M; ++n) {
+                    const int half = n / (2 * R), i = n % (2 * R) >> 1, nf = 2 * half + (n & 1);
+                    if (n == kFirst) {
+                        __builtin_amdgcn_sched_barrier(0);
+                        copies_landed<(kStages - 2) * T::kCopies>();
+                        next_sw = *reinterpret_cast<const float*>(st + at_sw);
+#pragma unroll
+                        for (int f = 0; f < R; ++f) next_sx[f] = *reinterpret_cast<const float*>(st + at_sx + f * 256);
+                        if (R > 1) {
+                            w[0] = weight_codes(st, 0);
+                            w[1] = weight_codes(st, 1);
+                        }
+                    }
+                    sums[n & 3] = multiply_codes(w[nf], x[i]);
+                    if (R == 1 && n < 2) w[n] = weight_codes(st, n);
+                    if (half == 1 && i == R - 1) w[nf] = weight_codes(st, nf);
+                    if (half == 1 && (n & 1)) x[i] = row_codes(st, i);
+                    constexpr int kPer = (T::kCopies + M - kFirst - 1) / (M - kFirst);
+#pragma unroll
+                    for (int c = 0; c < kPer; ++c)
+                        if (n >= kFirst) copy_piece((n - kFirst) * kPer + c);
+                    const int m = (n + M - 2) % M, m_half = m / (2 * R), m_i = m % (2 * R) >> 1;
+                    f32x4& sum = acc[2 * m_half + (m & 1)][m_i];
+                    const float scale = n < 2 ? last : by[m_i];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) sum[c] = fmaf(scale, sums[m & 3][c], sum[c]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                last = by[R - 1];
+#pragma unroll
+                for (int i = 0; i < R; ++i) by[i] = next_sx[i] * next_sw;
+            });
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) acc[2 + q][R - 1][c] = fmaf(last, sums[2 + q][c], acc[2 + q][R - 1][c]);
+        } else {
+            // A step is 2 R rounds of eight matrix instructions, two weight fragments x one row fragment.  What the vector unit has to do
+            // is spread between them, one piece after each: the codes of the next row fragment are widened, the sums of the round before
+            // are added to the accumulators; in the last round and in the next step's first one also the next stage's weights are widened,
+            // two fragments each, as their registers fall free.  The order is held by the scheduling barriers.
+            // At the beginning of a step: w[0], w[1] and the first row fragment widened, the codes of w[2], w[3] and half of the
+            // second row fragment's (if there is one), and the sums of the last round before it.
+            Widened w[4], x[2];
+            i32x8 codes_w[2], next_w[2];
+            i32x4 codes_x[2];                   // halves of the fragment that is widened next
+            f32x4 sums[2][2] = {};
+            float last_scale = 0.f;
+            const unsigned char* st0 = smem + slot * kStage;
+            w[0] = widen(weight_codes(st0, 0));
+            w[1] = widen(weight_codes(st0, 1));
+            codes_w[0] = weight_codes(st0, 2);
+            codes_w[1] = weight_codes(st0, 3);
+            x[0] = widen(row_codes(st0, 0));
+            codes_x[0] = row_codes_half(st0, 1, 0);
+            all_steps([&]() __attribute__((always_inline)) {
+                const unsigned char* st = smem + slot * kStage;
+                slot = slot == kStages - 1 ? 0 : slot + 1;
+                const unsigned char* st_next = smem + slot * kStage;
+                float scale[R];
+                const float sw = *reinterpret_cast<const float*>(st + at_sw);
+#pragma unroll
+                for (int i = 0; i < R; ++i) scale[i] = *reinterpret_cast<const float*>(st + at_sx + i * 256);
+#pragma unroll
+                for (int round = 0; round < 2 * R; ++round) {
+                    const int i = round >> 1, half = round & 1;
+                    if (round == (R > 2 ? 2 * R - 4 : 0)) {     // the next stage has landed, the one after it goes out
+                        __builtin_amdgcn_sched_barrier(0);
+                        copies_landed<(kStages - 3) * T::kCopies>();
+                        if (R == 1) codes_x[0] = row_codes_half(st_next, 0, 0);
+                    }
+                    // A round ahead of its use: the second half of the fragment that is widened now, the first half of the one after it.
+                    // Behind the last row fragment comes the next stage's first.
+                    if (half == 0) codes_x[1] = i + 1 < R ? row_codes_half(st, i + 1, 1) : row_codes_half(st_next, 0, 1);
+                    else if (R > 1) codes_x[0] = i + 2 < R ? row_codes_half(st, i + 2, 0) : row_codes_half(st_next, i + 2 - R, 0);
+                    if (half == 0 && i == R - 1) {
+                        next_w[0] = weight_codes(st_next, 0);
+                        next_w[1] = weight_codes(st_next, 1);
+                    }
+                    if (R == 1 && round == 1) {                 // one row fragment: their last use was a round ago
+                        w[2] = widen(codes_w[0]);
+                        w[3] = widen(codes_w[1]);
+                    }
+                    Widened& x_now = x[R > 1 ? i & 1 : 0];
+                    Widened& x_later = x[R > 1 ? (i & 1) ^ 1 : 1];
+                    const int before = round == 0 ? 2 * R - 1 : round - 1;      // the round whose sums are added
+                    const float by = round == 0 ? last_scale : scale[before >> 1] * sw;
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) {
+                        const int k = m >> 1, q = m & 1;
+                        f32x4& p = sums[round & 1][q];
+                        p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[2 * half + q].eight(k), x_now.eight(k),
+                                                                    k == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : p, 0, 0, 0);
+                        // one copy at a time: issued together they would hold up every wavefront
+                        constexpr int kFirst = R > 2 ? 8 * (2 * R - 4) : 0, kEvery = R == 1 ? 2 : 4;
+                        const int at = 8 * round + m - kFirst;
+                        if (at >= 0 && at % kEvery == 0) copy_piece(at / kEvery);
+                        x_later.widen_two(codes_x[half][m >> 1], half * 8 + m);
+                        f32x4& sum = acc[2 * (before & 1) + (m >> 2)][before >> 1];
+                        sum[m & 3] = fmaf(by, sums[(round & 1) ^ 1][m >> 2][m & 3], sum[m & 3]);
+                        if (R > 1 && round == 0) {
+#pragma unroll
+                            for (int c = 4 * m; c < 4 * m + 4; ++c) w[2 + (c >> 4)].widen_two(codes_w[c >> 4][(c & 15) >> 1], c & 15);
+                        }
+                        if (round == 2 * R - 1) {
+#pragma unroll
+                            for (int c = 4 * m; c < 4 * m + 4; ++c) w[c >> 4].widen_two(next_w[c >> 4][(c & 15) >> 1], c & 15);
+                            if (m == 4) codes_w[0] = weight_codes(st_next, 2);
+                            if (m == 7) codes_w[1] = weight_codes(st_next, 3);
+                        }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                }
+                last_scale = scale[R - 1] * sw;
+                if (R == 1) x[0] = x[1];
+            });
+#pragma unroll
+            for (int m = 0; m < 8; ++m)
+                acc[2 + (m >> 2)][R - 1][m & 3] = fmaf(last_scale, sums[1][m >> 2][m & 3], acc[2 + (m >> 2)][R - 1][m & 3]);
+        }
         const int lane = here(threadIdx.x) & 63, r = lane & 15;
         const int col0 = cur.group * kQuantBlock + wn * 64, first = wm * 16;            // this wavefront's columns and rows
         finish_values(a, cur.e, col0, acc);

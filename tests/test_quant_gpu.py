@@ -8,6 +8,10 @@ Tolerances, from the arithmetic and the formats (u = 2^-24, half a step of fp32)
     may truncate) of the sum of magnitudes off, scaling and adding up ceil(K / 128) blocks that many more, bias and the two scales'
     product 4: SUM(K) = (132 + ceil(K / 128)) 2^-23 of sum |a| |w| + |bias|.  GeLU has a slope of at most 1.13 and is itself
     within 1e-6 max(1, |z|) of 64 bits.
+    bf16 and e4m3 outputs may come from the matrix units for 8-bit operands, which add products in groups of eight and cut seven of them at
+    2^-13 of the largest one's power of two: at most 7 2^-13 of the sum of the groups' largest, so of sum |a| |w|.  The cuts go towards zero,
+    so with random signs they are independent, of mean 0 and a variance of at most 2^-26 / 3 of the largest one's square each; the groups'
+    largest squares add up to at most sum a^2 w^2: CUT = 8 standard deviations = 8 2^-13 sqrt(7 / 3 sum a^2 w^2), where that is less.
   rounding to the output: half a step, 2^-24 (fp32), 2^-8 (bf16), 2^-4 (e4m3; below 2^-6 times the scale 2^-10 times the scale), of a value that
     is itself off by the error above.
 """
@@ -34,6 +38,11 @@ def say(*a):
 
 def sum_error(K):
     return (132 + qo.blocks(K)) * 2.0 ** -23
+
+
+def cut_error(a, w):
+    """CUT of every row of `a` with every row of `w`."""
+    return np.minimum(7 * 2.0 ** -13 * (np.abs(a) @ np.abs(w).T), 8 * 2.0 ** -13 * np.sqrt(7 / 3 * ((a * a) @ (w * w).T)))
 
 
 def torch_dtype(name):
@@ -209,10 +218,12 @@ class Product:
     def weights(self, e):
         return self.w_codes[e] * qo.spread(self.w_scales[e].astype(np.float64), self.N, self.K)
 
-    def reference(self, rows, e, act, bias):
-        """(values, error bound of the fp32 result) of rows of `a` with matrix e."""
+    def reference(self, rows, e, act, bias, out):
+        """(values, error bound of the result before it is rounded to `out`) of rows of `a` with matrix e."""
         y, size = qo.linear(self.a[rows], self.weights(e), self.bias[e].astype(np.float64) if bias else None, act)
         err = sum_error(self.K) * size
+        if out != "f32":
+            err = err + cut_error(self.a[rows], self.weights(e))
         if act == "gelu":
             err = 1.13 * err + 1e-6 * np.maximum(1, size)
         return y, err
@@ -255,7 +266,7 @@ def test_linear(gpu_lib, T, N, K, out):
         y, sc = p.buffers(T, out, offset)
         moe.moe_quant_linear(shape, p.d_a, p.d_as, p.d_w, p.d_ws, torch.from_numpy(p.bias).cuda() if bias else None, y, sc, workspace(moe, shape))
         torch.cuda.synchronize()
-        check_rows(y, sc, *p.reference(slice(None), 0, act, bias), out)
+        check_rows(y, sc, *p.reference(slice(None), 0, act, bias, out), out)
 
 
 def grouped_case(p, sizes, k, rng):
@@ -310,7 +321,7 @@ def test_expert_linear(gpu_lib, name, out):
                 if mask is not None and not mask[e]:
                     assert torch.equal(y[s], before[0][s]) and (sc is None or torch.equal(sc[s], before[1][s]))
                     continue
-                check_rows(y[s], None if sc is None else sc[s], *p.reference(source[s], e, act, bias), out)
+                check_rows(y[s], None if sc is None else sc[s], *p.reference(source[s], e, act, bias, out), out)
 
 
 def test_bad_values_stay_where_they_are(gpu_lib):
@@ -359,8 +370,8 @@ def test_wrong_indices_stay_inside(gpu_lib):
                                 None, workspace(moe, shape))
     torch.cuda.synchronize()
     source = np.clip(perm, 0, A - 1)
-    check_rows(y[:10], None, *p.reference(source[:10], 0, "none", False), "f32")
-    check_rows(y[10:], None, *p.reference(source[10:], 1, "none", False), "f32")
+    check_rows(y[:10], None, *p.reference(source[:10], 0, "none", False, "f32"), "f32")
+    check_rows(y[10:], None, *p.reference(source[10:], 1, "none", False, "f32"), "f32")
 
 
 def test_rows_past_32_bits(gpu_lib):
@@ -383,7 +394,7 @@ def test_rows_past_32_bits(gpu_lib):
     moe.moe_quant_linear(shape, q, sc, packed, ws, None, y, None, workspace(moe, shape))
     a, b = VALUES[codes_of(q[pick])], VALUES[codes_of(w[0])]
     ref, size = qo.linear(a, b)
-    check_rows(y[pick], None, ref, sum_error(K) * size, "bf16")
+    check_rows(y[pick], None, ref, sum_error(K) * size + cut_error(a, b), "bf16")
     y[pick] = 0
     assert not y.any()
 
@@ -512,7 +523,7 @@ def test_moe_block(gpu_lib, T, d, f, E, k, H, act):
             assert np.isnan(y[s]).all()                     # not written
             continue
         v, size = qo.linear(a[perm[s] // k], unpacked(block.w1, e), block.b1[e].cpu().numpy().astype(np.float64), act)
-        err = sum_error(d) * size
+        err = sum_error(d) * size + cut_error(a[perm[s] // k], unpacked(block.w1, e))
         if act == "gelu":
             err = 1.13 * err + 1e-6 * np.maximum(1, size)
         assert_codes(codes_of(block.h8.codes[s]), block.h8.scales[s].cpu().numpy().astype(np.float64), v, err, f)
@@ -559,7 +570,9 @@ def test_dense_block(gpu_lib, T, d, f):
     out, _ = block.forward(x, r)
     torch.cuda.synchronize()
     check_norm(block, x, r, d)
-    v, size = qo.linear(row_values(block.x8, d), unpacked(block.w1, 0), block.b1.cpu().numpy().astype(np.float64), "relu")
-    assert_codes(codes_of(block.h8.codes), block.h8.scales.cpu().numpy().astype(np.float64), v, sum_error(d) * size, f)
-    v, size = qo.linear(row_values(block.h8, f), unpacked(block.w2, 0), block.b2.cpu().numpy().astype(np.float64))
-    check_rows(out, None, v, sum_error(f) * size, "bf16")
+    a, w = row_values(block.x8, d), unpacked(block.w1, 0)
+    v, size = qo.linear(a, w, block.b1.cpu().numpy().astype(np.float64), "relu")
+    assert_codes(codes_of(block.h8.codes), block.h8.scales.cpu().numpy().astype(np.float64), v, sum_error(d) * size + cut_error(a, w), f)
+    a, w = row_values(block.h8, f), unpacked(block.w2, 0)
+    v, size = qo.linear(a, w, block.b2.cpu().numpy().astype(np.float64))
+    check_rows(out, None, v, sum_error(f) * size + cut_error(a, w), "bf16")
