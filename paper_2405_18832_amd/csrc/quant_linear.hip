@@ -225,6 +225,15 @@ __device__ __forceinline__ void gather_columns(uint32_t (&v)[4]) {
     }
 }
 
+// Lane group g holds u = piece g of 32 columns' first half, v = of their second half (4 columns a piece); afterwards pieces 2 g, 2 g + 1 of
+// all 32, so that a store of 8 columns per lane covers 64 bytes of each row.
+__device__ __forceinline__ void gather_pair(uint32_t& u, uint32_t& v) {
+    const auto s = __builtin_amdgcn_permlane32_swap(u, v, false, false);
+    const auto t = __builtin_amdgcn_permlane16_swap(s[0], s[1], false, false);
+    u = t[0];
+    v = t[1];
+}
+
 template <int OUT, int STRIDE, int NF, int TF>
 __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row0, int rows, const f32x4 (&acc)[NF][TF]) {
     static_assert(OUT != kOutE4m3, "");
@@ -240,13 +249,16 @@ __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row
                 lo[nf] = pack_bf16x2(acc[nf % NF][tf][0], acc[nf % NF][tf][1]);
                 hi[nf] = pack_bf16x2(acc[nf % NF][tf][2], acc[nf % NF][tf][3]);
             }
-            gather_columns(lo);
-            gather_columns(hi);
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) {
+                gather_pair(lo[t], lo[t + 1]);
+                gather_pair(hi[t], hi[t + 1]);
+            }
             if (tf * STRIDE + r >= rows) continue;
-            const int n = n0 + g * 16;
+            const int n = n0 + g * 8;
             uint16_t* out = static_cast<uint16_t*>(a.out) + static_cast<size_t>(row0 + tf * STRIDE + r) * a.N + n;
             if (n < a.N) *reinterpret_cast<uint4*>(out) = uint4{lo[0], hi[0], lo[1], hi[1]};
-            if (n + 8 < a.N) *reinterpret_cast<uint4*>(out + 8) = uint4{lo[2], hi[2], lo[3], hi[3]};
+            if (n + 32 < a.N) *reinterpret_cast<uint4*>(out + 32) = uint4{lo[2], hi[2], lo[3], hi[3]};
         }
         return;
     }
@@ -277,7 +289,16 @@ __device__ __forceinline__ void store_values(const QuantArgs& a, int n0, int row
 // Largest magnitude of each row over the wavefront's columns that exist, for lane l of row 16 tf + l % 16.
 template <int NF, int TF>
 __device__ __forceinline__ void row_magnitudes(int N, int n0, f32x4 (&acc)[NF][TF], uint32_t (&most)[TF]) {
-    const int g = (here(threadIdx.x) & 63) >> 4;
+    if (n0 + NF * 16 > N) {                 // some do not exist
+        const int g = (here(threadIdx.x) & 63) >> 4;
+#pragma unroll
+        for (int tf = 0; tf < TF; ++tf)
+#pragma unroll
+            for (int nf = 0; nf < NF; ++nf)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n0 + nf * 16 + g * 4 + i >= N) acc[nf][tf][i] = 0.f;
+    }
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
         uint32_t m = 0;
@@ -285,7 +306,6 @@ __device__ __forceinline__ void row_magnitudes(int N, int n0, f32x4 (&acc)[NF][T
         for (int nf = 0; nf < NF; ++nf)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (n0 + nf * 16 + g * 4 + i >= N) acc[nf][tf][i] = 0.f;
                 m = max(m, magnitude(acc[nf][tf][i]));
             }
         m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
@@ -345,6 +365,14 @@ template <int LEFT>
 __device__ __forceinline__ void copies_landed() {
     static_assert(LEFT < 64, "vmcnt has six bits");
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(LEFT) : "memory");
+}
+// The same where `known` says (to the whole wavefront) that they have landed: no wait for what was issued since.  One block, so that no branch
+// of the compiler's divides a step.
+template <int LEFT>
+__device__ __forceinline__ void copies_landed_unless(uint32_t known) {
+    static_assert(LEFT < 64, "vmcnt has six bits");
+    asm volatile("s_cmp_lg_u32 %0, 0\n\ts_cbranch_scc1 .Lknown%=\n\ts_waitcnt vmcnt(%1)\n.Lknown%=:\n\ts_waitcnt lgkmcnt(0)\n\ts_barrier"
+                 : : "s"(uniform(static_cast<int>(known))), "n"(LEFT) : "memory", "scc");
 }
 __device__ __forceinline__ i32x8 read_codes(const unsigned char* p, int other) {
     const i32x4 lo = *reinterpret_cast<const i32x4*>(p), hi = *reinterpret_cast<const i32x4*>(p + other);
@@ -868,6 +896,7 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
     }
 
     int slot = 0;
+    uint32_t landed = 0;                    // steps from here on whose next stage is known to have landed
     auto run_unit = [&](auto fragments) __attribute__((always_inline)) {
         constexpr int R = decltype(fragments)::value;
         const int tid = here(threadIdx.x);
@@ -892,6 +921,7 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
                 kb_in = uniform(kb_in);
                 slot_in = uniform(slot_in);
                 slot = uniform(slot);
+                landed = uniform(landed);
                 stage_step = uniform(stage_step);
                 weights_base = uniform(weights_base);
                 if constexpr (OFFSETS) {
@@ -901,6 +931,8 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
                 const int steps = min(KB - j, KB - kb_in);
                 j += steps;
                 kb_in += steps;
+                // nothing pending on the way in (lgkmcnt(0), the compiler counts with it): the steps wait only for what they read themselves
+                __builtin_amdgcn_s_waitcnt(0xc07f);
 #pragma unroll 1
                 for (int s = 0; s < steps; ++s) {
                     step();
@@ -913,10 +945,10 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
             // A step is 4 R matrix instructions: the first two weight fragments x every row fragment, then the other two.  Operands are
             // read from the next stage into the registers of those that were used last, at least 2 R + 1 instructions (2 of one row
             // fragment) before their use; a stage's slot is free again in the middle of its own step, so that a copy has two steps to
-            // land in.  A sum is added to its accumulator two instructions after its own.  The order is held by the scheduling barriers.
+            // land in.  A sum is added to its accumulator three instructions after its own.  The order is held by the scheduling barriers.
             i32x8 w[4], x[R];
             f32x4 sums[4] = {};
-            float by[R], last = 0.f;
+            float by[R], last[R] = {};
             const unsigned char* st0 = smem + slot * kStage;
 #pragma unroll
             for (int nf = 0; nf < 4; ++nf) w[nf] = weight_codes(st0, nf);
@@ -934,7 +966,8 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
                     const int half = n / (2 * R), i = n % (2 * R) >> 1, nf = 2 * half + (n & 1);
                     if (n == kFirst) {
                         __builtin_amdgcn_sched_barrier(0);
-                        copies_landed<(kStages - 2) * T::kCopies>();
+                        copies_landed_unless<(kStages - 2) * T::kCopies>(landed);
+                        landed = landed > 0 ? landed - 1 : 0;
                         next_sw = *reinterpret_cast<const float*>(st + at_sw);
 #pragma unroll
                         for (int f = 0; f < R; ++f) next_sx[f] = *reinterpret_cast<const float*>(st + at_sx + f * 256);
@@ -944,6 +977,7 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
                         }
                     }
                     sums[n & 3] = multiply_codes(w[nf], x[i]);
+                    __builtin_amdgcn_sched_barrier(0);
                     if (R == 1 && n < 2) w[n] = weight_codes(st, n);
                     if (half == 1 && i == R - 1) w[nf] = weight_codes(st, nf);
                     if (half == 1 && (n & 1)) x[i] = row_codes(st, i);
@@ -951,21 +985,30 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
 #pragma unroll
                     for (int c = 0; c < kPer; ++c)
                         if (n >= kFirst) copy_piece((n - kFirst) * kPer + c);
-                    const int m = (n + M - 2) % M, m_half = m / (2 * R), m_i = m % (2 * R) >> 1;
+                    const int m = (n + M - 3) % M, m_half = m / (2 * R), m_i = m % (2 * R) >> 1;
                     f32x4& sum = acc[2 * m_half + (m & 1)][m_i];
-                    const float scale = n < 2 ? last : by[m_i];
+                    const float scale = n < 3 ? last[m_i] : by[m_i];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) sum[c] = fmaf(scale, sums[m & 3][c], sum[c]);
                     __builtin_amdgcn_sched_barrier(0);
                 }
-                last = by[R - 1];
 #pragma unroll
-                for (int i = 0; i < R; ++i) by[i] = next_sx[i] * next_sw;
+                for (int i = 0; i < R; ++i) {
+                    last[i] = by[i];
+                    by[i] = next_sx[i] * next_sw;
+                }
             });
 #pragma unroll
-            for (int q = 0; q < 2; ++q)
+            for (int m = 4 * R - 3; m < 4 * R; ++m) {
+                const int i = m % (2 * R) >> 1;
+                f32x4& sum = acc[2 * (m / (2 * R)) + (m & 1)][i];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[2 + q][R - 1][c] = fmaf(last, sums[2 + q][c], acc[2 + q][R - 1][c]);
+                for (int c = 0; c < 4; ++c) sum[c] = fmaf(last[i], sums[m & 3][c], sum[c]);
+            }
+            // The stores below are counted behind the copies in flight, which have landed when they go out; so the next unit's first steps need
+            // not wait for stores.
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            landed = kStages - 1;
         } else {
             // A step is 2 R rounds of eight matrix instructions, two weight fragments x one row fragment.  What the vector unit has to do
             // is spread between them, one piece after each: the codes of the next row fragment are widened, the sums of the round before
