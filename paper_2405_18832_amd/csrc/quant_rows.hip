@@ -12,11 +12,14 @@ namespace moe {
 // A lane holds chunks of 8 consecutive values, so that 16 lanes are a block of 128 (its maximum takes four DPP rotations) and a
 // wavefront covers 512 values per chunk; chunk c of a row is done by wavefront c % WPR of the row's WPR wavefronts.
 
+// 16 bytes at an address that is a multiple of the element's size only: one access all the same, as the machine takes them
+typedef __attribute__((ext_vector_type(4), aligned(2))) uint32_t any_u32x4;
+typedef __attribute__((ext_vector_type(4), aligned(4))) float any_f32x4;
+
 template <typename ST> struct Eight;
 template <> struct Eight<uint16_t> {
     static __device__ __forceinline__ void load(const uint16_t* p, float (&v)[8]) {
-        const uint4 u = *reinterpret_cast<const uint4*>(p);
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        const any_u32x4 w = *reinterpret_cast<const any_u32x4*>(p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[2 * i] = __uint_as_float(w[i] << 16);
@@ -24,14 +27,14 @@ template <> struct Eight<uint16_t> {
         }
     }
     static __device__ __forceinline__ void store(uint16_t* p, const float (&v)[8]) {
-        *reinterpret_cast<uint4*>(p) =
-            uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        *reinterpret_cast<any_u32x4*>(p) =
+            any_u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
     }
     static __device__ __forceinline__ float round(float v) { return bf16_to_f32(f32_to_bf16(v)); }
 };
 template <> struct Eight<float> {
     static __device__ __forceinline__ void load(const float* p, float (&v)[8]) {
-        const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 4);
+        const any_f32x4 a = *reinterpret_cast<const any_f32x4*>(p), b = *reinterpret_cast<const any_f32x4*>(p + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             v[i] = a[i];
@@ -39,16 +42,16 @@ template <> struct Eight<float> {
         }
     }
     static __device__ __forceinline__ void store(float* p, const float (&v)[8]) {
-        *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        *reinterpret_cast<any_f32x4*>(p) = any_f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<any_f32x4*>(p + 4) = any_f32x4{v[4], v[5], v[6], v[7]};
     }
     static __device__ __forceinline__ float round(float v) { return v; }
 };
 
-// 8 values from column `c` of a row of d; those past the end are zero.  VEC: whole chunks only, 16-byte aligned.
-template <typename ST, bool VEC>
+// 8 values from column `c` of a row of d; those past the end are zero.  WHOLE: d is a multiple of 8, no row ends inside a chunk.
+template <typename ST, bool WHOLE>
 __device__ __forceinline__ void load8(const ST* row, int c, int d, float (&v)[8]) {
-    if constexpr (VEC) {
+    if constexpr (WHOLE) {
         if (c < d) {
             Eight<ST>::load(row + c, v);
             return;
@@ -56,15 +59,23 @@ __device__ __forceinline__ void load8(const ST* row, int c, int d, float (&v)[8]
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = 0.f;
     } else {
+        if (c + 8 <= d) {
+            Eight<ST>::load(row + c, v);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = c + i < d ? Storage<ST>::load(row + c + i) : 0.f;
     }
 }
-template <typename ST, bool VEC>
+template <typename ST, bool WHOLE>
 __device__ __forceinline__ void store8(ST* row, int c, int d, const float (&v)[8]) {
-    if constexpr (VEC) {
+    if constexpr (WHOLE) {
         if (c < d) Eight<ST>::store(row + c, v);
     } else {
+        if (c + 8 <= d) {
+            Eight<ST>::store(row + c, v);
+            return;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (c + i < d) Storage<ST>::store(row + c + i, v[i]);
@@ -133,7 +144,7 @@ struct NormArgs {
 };
 
 // NV: chunks that a wavefront keeps in registers; 0: rows longer than any variant keeps, which are read a second time.
-template <typename ST, int WPR, int NV, bool VEC>
+template <typename ST, int WPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(kNormWaves * 64) void norm_quantize_kernel(const NormArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = wave % WPR;
@@ -151,10 +162,10 @@ __global__ __launch_bounds__(kNormWaves * 64) void norm_quantize_kernel(const No
     const int chunks = (static_cast<int>(pitch) + kNormValues - 1) / kNormValues;
     auto column = [&](int chunk) { return chunk * kNormValues + lane * 8; };
     auto read_sum = [&](int chunk, float (&s)[8]) {
-        load8<ST, VEC>(x, column(chunk), d, s);
+        load8<ST, WHOLE>(x, column(chunk), d, s);
         if (res != nullptr) {
             float r[8];
-            load8<ST, VEC>(res, column(chunk), d, r);
+            load8<ST, WHOLE>(res, column(chunk), d, r);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s[i] = Eight<ST>::round(s[i] + r[i]);
         }
@@ -203,17 +214,17 @@ __global__ __launch_bounds__(kNormWaves * 64) void norm_quantize_kernel(const No
 
     auto finish = [&](int chunk, float (&s)[8]) {
         const int c = column(chunk);
-        if (sum_out != nullptr) store8<ST, VEC>(sum_out, c, d, s);
+        if (sum_out != nullptr) store8<ST, WHOLE>(sum_out, c, d, s);
         uint32_t most = 0;
         float w[8], n[8];
-        if (a.weight != nullptr) load8<float, VEC>(a.weight, c, d, w);
+        if (a.weight != nullptr) load8<float, WHOLE>(a.weight, c, d, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             n[i] = s[i] * rho;
             if (a.weight != nullptr) n[i] *= w[i];
             most = max(most, c + i < d ? magnitude(n[i]) : 0u);
         }
-        if (norm_out != nullptr) store8<ST, VEC>(norm_out, c, d, n);
+        if (norm_out != nullptr) store8<ST, WHOLE>(norm_out, c, d, n);
         most = row16_max(most);
         const float scale = block_scale(most), inv = 1.f / scale;
         bool unsure = false;
@@ -240,7 +251,7 @@ __global__ __launch_bounds__(kNormWaves * 64) void norm_quantize_kernel(const No
     }
 }
 
-template <typename ST, bool VEC>
+template <typename ST, bool WHOLE>
 static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
     const int chunks = static_cast<int>((quant_pitch(a.d) + kNormValues - 1) / kNormValues);
     const dim3 block(kNormWaves * 64);
@@ -248,22 +259,22 @@ static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
         const int per_block = kNormWaves / wpr;
         kernel<<<dim3((a.rows + per_block - 1) / per_block), block, 0, stream>>>(a);
     };
-    if (chunks <= kNormWaves) go(norm_quantize_kernel<ST, 4, 1, VEC>, 4);
-    else if (chunks <= 2 * kNormWaves) go(norm_quantize_kernel<ST, 4, 2, VEC>, 4);
-    else if (chunks <= 8 * kNormWaves) go(norm_quantize_kernel<ST, 4, 8, VEC>, 4);
-    else go(norm_quantize_kernel<ST, 4, 0, VEC>, 4);
+    // as many wavefronts per row as it has chunks
+    if (chunks == 1) go(norm_quantize_kernel<ST, 1, 1, WHOLE>, 1);
+    else if (chunks == 2) go(norm_quantize_kernel<ST, 2, 1, WHOLE>, 2);
+    else if (chunks <= kNormWaves) go(norm_quantize_kernel<ST, 4, 1, WHOLE>, 4);
+    else if (chunks <= 2 * kNormWaves) go(norm_quantize_kernel<ST, 4, 2, WHOLE>, 4);
+    else if (chunks <= 8 * kNormWaves) go(norm_quantize_kernel<ST, 4, 8, WHOLE>, 4);
+    else go(norm_quantize_kernel<ST, 4, 0, WHOLE>, 4);
     return hipGetLastError();
 }
 
 hipError_t launch_norm_quantize(int rows, int d, int dtype, const void* x, const void* residual, const float* weight, float eps,
                                 void* sum_out, void* norm_out, uint8_t* q, float* q_scales, hipStream_t stream) {
     const NormArgs a{x, residual, weight, eps, sum_out, norm_out, q, q_scales, rows, d};
-    uintptr_t all = 0;
-    for (const void* p : {x, residual, static_cast<const void*>(weight), static_cast<const void*>(sum_out), static_cast<const void*>(norm_out)})
-        all |= reinterpret_cast<uintptr_t>(p);
-    const bool vec = d % 8 == 0 && all % 16 == 0;
-    if (dtype == MOE_BF16) return vec ? launch_norm<uint16_t, true>(a, stream) : launch_norm<uint16_t, false>(a, stream);
-    return vec ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
+    const bool whole = d % 8 == 0;
+    if (dtype == MOE_BF16) return whole ? launch_norm<uint16_t, true>(a, stream) : launch_norm<uint16_t, false>(a, stream);
+    return whole ? launch_norm<float, true>(a, stream) : launch_norm<float, false>(a, stream);
 }
 
 // ---- moe_quantize_weights -------------------------------------------------------------------------------------------
