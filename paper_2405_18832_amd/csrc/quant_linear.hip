@@ -390,7 +390,8 @@ __device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
 // Unit: an expert's rows, at most 64, x 128 NF columns, by 8 wavefronts of 16 NF columns each, a block of 128 columns of the contraction
-// per step.  Bound by memory, so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
+// per step.  Bound by memory (49 experts of one to three rows, 2048 x 8192: 142 us = 5.9 TB/s; 64 experts of 32 rows, 3072 x 768: 37 us =
+// 4.1 TB/s, 3 of them for the launch), so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
 // through a ring of stages that runs on across units.  A block's units follow each other in one expert, where nothing needs to be looked
 // up (a load that the compiler sees would make it wait for every copy in flight).
 constexpr int kStreamRows = 64, kStreamWaves = 8;
@@ -739,6 +740,14 @@ __global__ __launch_bounds__(256) void quant_join_kernel(const QuantArgs a, cons
 //   weights  8 fragments of 2 KiB as they are packed, 16 rows each
 //   scales   of the rows, and the weights' (one for the unit's 128 columns)
 // Wavefront (wm, wn) of the 4 x 2 multiplies row fragments wm, wm + 4, ... (R of them) and the columns 64 wn ... 64 wn + 63.
+//
+// What bounds it, with the 8-bit units (16384 x 8192 x 8192, bf16 out: 1054 us = 2090 TFLOP/s; x 2048: 295 us = 1860; a library product
+// with one scale per operand, 16384 x 8192 x 2048: 254 us): the power limit, under which the clock falls to 1.4 to 1.8 GHz, and the copies.  A
+// copy of this kernel without the copies took 771 us, without the LDS reads 1045, with neither 698, without the multiply-adds 1058; copying
+// one stage over and over 1043, so that it is not the distance to the memory.  Units of 256 x 256, which copy a third less per product, took 1064
+// us, and 349 instead of 307 for 2048 columns of contraction: the next unit's copies have half the time, twice the sums are finished at once
+// and registers run out there.  Finishing and storing is 37 us of the 295, GeLU 45 more.  With the bf16 units (fp32 out, 16384 x 2048 x 8192:
+// 460 us = 1200 TFLOP/s) the vector unit is the bound, which widens 128 x 64 codes per matrix unit and step.
 constexpr int kTileWaves = 8;
 template <int RMAX>
 struct Tiles {
@@ -1161,9 +1170,12 @@ size_t quant_product_workspace(const moe_quant_shape& s) {
 }
 
 // Row fragments per wavefront of the tiled kernel, so rows per tile / 64: large tiles do more per byte and per conversion, small ones
-// occupy more CUs.  A step of 256, 128 and 64 rows takes 1.95, 1.2 and 0.8 us on a CU; a unit of each kind has as many steps as the
-// other, so what counts is rounds of 256 units times that.  (1501 rows x 768 x 3072 54.6, 37.0 and 26.2 us; 16384 x 8192 x 2048 542, 671
-// and 988.)  A grouped call's last tiles are not known here and left out.  Tiles of 256 rows address the rows by 32-bit offsets.
+// occupy more CUs.  A step of 256, 128 and 64 rows takes 1.95, 1.2 and 0.8 us on a CU with the bf16 units, 0.95, 0.7 and 0.6 with the 8-bit
+// ones; a unit of each kind has as many steps as the other, so what counts is rounds of 256 units times that.  The ratios of the first three are
+// taken for both: with each kind forced, the choice was the fastest one or within 5 % of it for each of 22 shapes of 200 to 8000 rows
+// (64, 128, 256 rows, us; bf16 out: 1501 x 768 x 3072 16.0, 21.3, 30.1; 4096 x 1024 x 4096 31.8, 26.9, 41.0; 2048 x 8192 x 2048 65.4,
+// 53.0, 45.5; fp32 out: 25.4, 33.4, 46.9; 54.1, 41.7, 64.5; 109, 84, 74).  A grouped call's last tiles are not known here and left out.
+// Tiles of 256 rows address the rows by 32-bit offsets.
 static int tile_fragments(int rows, int N, size_t operand_bytes) {
     auto cost = [&](int r, float step) {
         const long long units = static_cast<long long>((rows + 64 * r - 1) / (64 * r)) * quant_blocks(N);
