@@ -166,20 +166,15 @@ def _nbytes(t) -> int:
     return 0 if t is None else t.numel() * t.element_size()
 
 
-_raw_stream = None      # torch's own calls for the current device and its current stream's handle, looked up once
-
-
 def _stream(stream) -> Optional[int]:
-    global _raw_stream
     if stream is None:
-        if _raw_stream is None:
-            import torch
-            # the handle itself: building a torch.cuda.Stream around it takes 2.7 us, a tenth of a small layer's host time; these
-            # calls are not part of torch's public interface, so a torch without them goes the long way
-            raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-            torch.cuda.current_device()         # initialises torch's side
-            _raw_stream = (lambda: raw(device())) if raw is not None and device is not None else lambda: torch.cuda.current_stream().cuda_stream
-        return _raw_stream() or None
+        import torch
+        # the handle itself: building a torch.cuda.Stream around it takes 2.7 us, a tenth of a small layer's host time; the
+        # call is not part of torch's public interface, so a torch without it goes the long way
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None:
+            return raw(torch.cuda.current_device()) or None
+        stream = torch.cuda.current_stream()
     if isinstance(stream, int):
         return stream or None
     return stream.cuda_stream or None
