@@ -192,6 +192,26 @@ def test_weights(gpu_lib, E, N, K):
             assert ((c >= lo) & (c <= hi)).all()
 
 
+@pytest.mark.parametrize("dtype", ["e4m3", "bf16", "f32"])
+@pytest.mark.parametrize("N,K", [(130, 200), (128, 256), (17, 131)])
+def test_weights_from_any_address(gpu_lib, N, K, dtype):
+    """Weights that begin on a multiple of their element's size only."""
+    moe = gpu_lib
+    say(f"[case] moe_quantize_weights from odd addresses {N} x {K} {dtype}")
+    w = torch.randn((2, N, K), device="cuda", generator=torch.Generator(device="cuda").manual_seed(N + K))
+    w = w.to(torch.float8_e4m3fn).view(torch.uint8) if dtype == "e4m3" else w.to(torch_dtype(dtype))
+    got = []
+    for offset in (0, 1, 3):
+        src = torch.empty(w.numel() + offset, dtype=w.dtype, device="cuda")[offset:].view(w.shape)
+        src.copy_(w)
+        dst = torch.full((moe.moe_quant_weight_bytes(2, N, K),), 0x55, dtype=torch.uint8, device="cuda")
+        sc = None if dtype == "e4m3" else torch.full((2, qo.blocks(N), qo.blocks(K)), -1.0, device="cuda")
+        moe.moe_quantize_weights(2, N, K, dtype, src, dst, sc)
+        got.append((dst, sc))
+    for dst, sc in got[1:]:
+        assert torch.equal(dst, got[0][0]) and (sc is None or torch.equal(sc, got[0][1]))
+
+
 # ---- products -------------------------------------------------------------------------------------------------------
 class Product:
     """Seeded operands of a product, their values for the reference and their device copies."""
@@ -322,6 +342,46 @@ def test_expert_linear(gpu_lib, name, out):
                     assert torch.equal(y[s], before[0][s]) and (sc is None or torch.equal(sc[s], before[1][s]))
                     continue
                 check_rows(y[s], None if sc is None else sc[s], *p.reference(source[s], e, act, bias, out), out)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("T,N,K", [(3, 256, 1024), (60, 200, 300), (300, 384, 640), (5000, 2048, 300)])
+def test_outlier_columns(gpu_lib, T, N, K, out):
+    """One column of every block a hundred times the others, as activations have them: what a matrix unit may cut is largest there."""
+    moe = gpu_lib
+    say(f"[case] outlier columns {T} x {N} x {K} {out}")
+    p = Product(moe, T, N, K)
+    a = p.rng.standard_normal((T, K))
+    a[:, 5::128] *= 100
+    q, s = qo.quantize_rows(a)
+    p.a_scales = s.astype(np.float32)
+    p.a = qo.dequantize_rows(q, p.a_scales.astype(np.float64))
+    padded = np.zeros((T, moe.moe_quant_pitch(K)), dtype=np.float32)
+    padded[:, :K] = q
+    p.d_a, p.d_as = torch.from_numpy(padded).cuda().to(torch.float8_e4m3fn), torch.from_numpy(p.a_scales).cuda()
+    shape = moe.make_quant_shape(T, N, K, 1, 1, "none", out)
+    y, sc = p.buffers(T, out)
+    moe.moe_quant_linear(shape, p.d_a, p.d_as, p.d_w, p.d_ws, None, y, sc, workspace(moe, shape))
+    torch.cuda.synchronize()
+    check_rows(y, sc, *p.reference(slice(None), 0, "none", False, out), out)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("rows", [5, 64, 900])
+def test_nothing_to_do(gpu_lib, rows, out):
+    """Every expert masked out, and rows that are no expert's: nothing is written."""
+    moe = gpu_lib
+    say(f"[case] no expert runs, {rows} rows {out}")
+    E, N, K = 3, 256, 200
+    p = Product(moe, rows, N, K, E)
+    shape = moe.make_quant_shape(rows, N, K, E, 1, "relu", out)
+    cut = torch.tensor([0, rows // 2, rows // 2, rows], dtype=torch.int32, device="cuda")
+    for offsets, mask in ((cut, torch.zeros(E, dtype=torch.uint8, device="cuda")), (torch.zeros_like(cut), None)):
+        y, sc = p.buffers(rows, out)
+        before = (y.clone(), None if sc is None else sc.clone())
+        moe.moe_quant_expert_linear(shape, p.d_a, p.d_as, None, offsets, mask, p.d_w, p.d_ws, None, y, sc, workspace(moe, shape))
+        torch.cuda.synchronize()
+        assert torch.equal(y, before[0]) and (sc is None or torch.equal(sc, before[1]))
 
 
 def test_bad_values_stay_where_they_are(gpu_lib):
