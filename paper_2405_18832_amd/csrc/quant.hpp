@@ -59,6 +59,7 @@ struct QuantArgs {
     void* out;
     float* out_scales;
     int rows, N, K, E, k, act, out_dtype;
+    bool once = false;          // streamed weights are not kept in the caches
 };
 
 // csrc/quant_rows.hip

@@ -351,6 +351,11 @@ __device__ __forceinline__ void copy4_to_lds(const void* src, uint32_t lds_base)
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(dst) : "memory");
 }
+// copy16_to_lds of what is read once: the lines are the first to leave the caches
+__device__ __forceinline__ void copy16_once_to_lds(const void* src, uint32_t lds_base) {
+    const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" : : "v"(src), "s"(dst) : "memory");
+}
 // The same from 32-bit offsets to a base that is the same for the whole wavefront: half the registers, and the base moves on for free
 __device__ __forceinline__ void copy16_to_lds(const void* base, uint32_t offset, uint32_t lds_base) {
     const uint32_t dst = __builtin_amdgcn_readfirstlane(lds_base);
@@ -390,8 +395,8 @@ __device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
 // Unit: an expert's rows, at most 64, x 128 NF columns, by 8 wavefronts of 16 NF columns each, a block of 128 columns of the contraction
-// per step.  Bound by memory (49 experts of one to three rows, 2048 x 8192: 142 us = 5.9 TB/s; 64 experts of 32 rows, 3072 x 768: 37 us =
-// 4.1 TB/s, 3 of them for the launch), so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
+// per step.  Bound by memory (49 experts of one to three rows, 2048 x 8192: 136 to 140 us = 6.1 to 6.3 TB/s; 64 experts of 32 rows, 3072 x
+// 768: 35 us = 4.3 TB/s, 3 of them for the launch), so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
 // through a ring of stages that runs on across units.  A block's units follow each other in one expert, where nothing needs to be looked
 // up (a load that the compiler sees would make it wait for every copy in flight).
 constexpr int kStreamRows = 64, kStreamWaves = 8;
@@ -509,12 +514,16 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int tiles, int 
     };
     auto stage_in = [&](int slot) {
         const int at = slot * kStage;
+        auto weights = [&](auto copy) __attribute__((always_inline)) {
 #pragma unroll
-        for (int nf = 0; nf < NF; ++nf) {
-            const uint8_t* from = weights_from + static_cast<size_t>(nf) * KB * kFragBytes;
-            copy16_to_lds(from, to_weights + at + nf * kFragBytes);
-            copy16_to_lds(from + 1024, to_weights + at + nf * kFragBytes + 1024);
-        }
+            for (int nf = 0; nf < NF; ++nf) {
+                const uint8_t* from = weights_from + static_cast<size_t>(nf) * KB * kFragBytes;
+                copy(from, to_weights + at + nf * kFragBytes);
+                copy(from + 1024, to_weights + at + nf * kFragBytes + 1024);
+            }
+        };
+        if (a.once) weights([](const void* from, uint32_t to) __attribute__((always_inline)) { copy16_once_to_lds(from, to); });
+        else weights([](const void* from, uint32_t to) __attribute__((always_inline)) { copy16_to_lds(from, to); });
         copy16_to_lds(row_from, to_rows + at);
         copy4_to_lds(scales_from, to_scales + at);
         weights_from += kFragBytes;
@@ -1242,7 +1251,15 @@ hipError_t configure_quant_kernels() {
     return hipSuccess;
 }
 
-hipError_t launch_quant_product(const QuantArgs& a, void* ws, hipStream_t stream) {
+// Weights that do not fit the L2s (8 x 4 MiB) are gone before the next call reads them: streamed units then read them as what is read once,
+// and leave the caches to the rows (Switch-base pair with its combine 81.6 -> 77.0 us, 16384 skewed tokens 1037 -> 1020; 32 tokens of 128
+// experts, 2048 x 8192, where runs of one build differ by 10 %, 136 to 150 -> 133 to 140).  A
+// matrix that fits may still be there (32 x 8192 x 2048, 17 MB, called again and again: 10.8 us, read as once 12.0).
+constexpr size_t kCachedWeights = size_t{32} << 20;
+
+hipError_t launch_quant_product(const QuantArgs& args, void* ws, hipStream_t stream) {
+    QuantArgs a = args;
+    a.once = a.E * quant_matrix_bytes(a.N, a.K) > kCachedWeights;
     if (a.out_dtype == MOE_F32) return launch_out<kOutF32>(a, ws, stream);
     if (a.out_dtype == MOE_BF16) return launch_out<kOutBf16>(a, ws, stream);
     return launch_out<kOutE4m3>(a, ws, stream);
