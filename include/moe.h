@@ -372,19 +372,26 @@ typedef struct {
     int32_t E;            /* weight matrices; 1 for moe_quant_linear                                    */
     int32_t k;            /* with a `perm`: assignments per token, rows % k == 0 (else 1)                */
     int32_t activation;   /* moe_activation                                                             */
-    int32_t out_dtype;    /* MOE_F32, MOE_BF16: [rows, N], last index contiguous; MOE_E4M3: quantised rows */
+    int32_t out_dtype;    /* MOE_F32, MOE_BF16: [rows, N], last index contiguous; MOE_E4M3: quantised rows;
+                             the last two also with MOE_QUANT_UNIT_SUMS                          */
 } moe_quant_shape;
+
+/*
+ * MOE_BF16 | MOE_QUANT_UNIT_SUMS, MOE_E4M3 | MOE_QUANT_UNIT_SUMS as an out_dtype: the sums within a block of 128 may come from the matrix
+ * units for 8-bit operands.  They add products in groups of eight, cut at 2^-13 of the power of two of the group's largest: 1.5e-5 of the
+ * rms of a sum of normal values, at most 7 * 2^-13 of the sum of magnitudes, so that what is left where large products cancel may be lost.
+ * Calls of many rows take up to two thirds of the time that fp32 sums take.  Calls of few rows whose contraction is cut have fp32 sums all the same.
+ */
+#define MOE_QUANT_UNIT_SUMS 0x100
 
 /* Bytes of workspace of the two calls below (0 on a shape that they refuse). */
 size_t moe_quant_workspace_bytes(const moe_quant_shape* shape);
 
 /*
  * out[r, n] = act( sum_b sa[r, b] * sw[n/128, b] * sum_{c in block b} a[r, c] * w[n, c] + bias[n] )
- * a, sa: quantised rows [rows, K]; w, sw: packed weights and their scales (E = 1); bias [N] fp32 or NULL.  The blocks' sums are added up in
- * fp32 and the result is rounded once, to out_dtype.  For an out_dtype of MOE_F32 the sums within a block are fp32 as well; for the others they
- * may come from the matrix units for 8-bit operands, which cut products at 2^-13 of the largest of each eight (1.5e-5 of the rms of a sum
- * of normal values).  out_scales: scales of the quantised output, NULL for the
- * other types.  ws: at least moe_quant_workspace_bytes, 256-byte aligned.  Outputs overlap nothing.
+ * a, sa: quantised rows [rows, K]; w, sw: packed weights and their scales (E = 1); bias [N] fp32 or NULL.  Sums are fp32 (unless the caller
+ * asks for MOE_QUANT_UNIT_SUMS), within a block and over the blocks, and the result is rounded once, to out_dtype.  out_scales: scales of the
+ * quantised output, NULL for the other types.  ws: at least moe_quant_workspace_bytes, 256-byte aligned.  Outputs overlap nothing.
  */
 moe_status moe_quant_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const void* w, const float* w_scales,
                             const float* bias, void* out, float* out_scales, void* ws, size_t ws_bytes, void* stream);

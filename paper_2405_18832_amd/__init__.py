@@ -20,6 +20,7 @@ MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP
 MOE_F32, MOE_BF16, MOE_E4M3 = 0, 1, 2
 MOE_ACT_NONE, MOE_ACT_RELU, MOE_ACT_GELU = -1, 0, 1
 MOE_QUANT_BLOCK = 128
+MOE_QUANT_UNIT_SUMS = 0x100
 MOE_MAX_K, MOE_MAX_E = 8, 1024
 
 EXPORTS = ["moe_init", "moe_noalloc_max_workspace", "moe_layer_forward_noalloc",
@@ -143,10 +144,11 @@ _DTYPE_NAMES = {"f32": MOE_F32, "bf16": MOE_BF16, "e4m3": MOE_E4M3}
 _ACT_NAMES = {"none": MOE_ACT_NONE, "relu": MOE_ACT_RELU, "gelu": MOE_ACT_GELU}
 
 
-def make_quant_shape(rows, N, K, E=1, k=1, activation="none", out_dtype="bf16") -> moe_quant_shape:
-    """`activation`: "none" | "relu" | "gelu", `out_dtype`: "f32" | "bf16" | "e4m3" (or the C values)."""
-    return moe_quant_shape(int(rows), int(N), int(K), int(E), int(k), int(_ACT_NAMES.get(activation, activation)),
-                           int(_DTYPE_NAMES.get(out_dtype, out_dtype)))
+def make_quant_shape(rows, N, K, E=1, k=1, activation="none", out_dtype="bf16", sums="f32") -> moe_quant_shape:
+    """`activation`: "none" | "relu" | "gelu", `out_dtype`: "f32" | "bf16" | "e4m3" (or the C values).  `sums`: "f32", or "units" for sums by
+    the matrix units for 8-bit operands (MOE_QUANT_UNIT_SUMS: faster for many rows, less exact; bf16 and e4m3 outputs)."""
+    out = int(_DTYPE_NAMES.get(out_dtype, out_dtype)) | {"f32": 0, "units": MOE_QUANT_UNIT_SUMS}[sums]
+    return moe_quant_shape(int(rows), int(N), int(K), int(E), int(k), int(_ACT_NAMES.get(activation, activation)), out)
 
 
 def _ptr(t) -> Optional[int]:

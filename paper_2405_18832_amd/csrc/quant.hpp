@@ -59,6 +59,7 @@ struct QuantArgs {
     void* out;
     float* out_scales;
     int rows, N, K, E, k, act, out_dtype;
+    bool unit_sums;             // blocks' sums by the matrix units for 8-bit operands
     bool once = false;          // streamed weights are not kept in the caches
 };
 

@@ -16,11 +16,14 @@ moe_status check_matrices(int32_t E, int32_t N, int32_t K) {
     return MOE_OK;
 }
 
+int out_type(const moe_quant_shape& s) { return s.out_dtype & ~MOE_QUANT_UNIT_SUMS; }
+
 moe_status check_product(const moe_quant_shape* s) {
     if (s == nullptr || s->rows < 0 || s->k < 1) return MOE_ERR_INVALID_ARG;
     const moe_status st = check_matrices(s->E, s->N, s->K);
     if (st != MOE_OK) return st;
-    if (s->out_dtype != MOE_F32 && s->out_dtype != MOE_BF16 && s->out_dtype != MOE_E4M3) return MOE_ERR_INVALID_ARG;
+    const int out = out_type(*s);
+    if (out != MOE_BF16 && out != MOE_E4M3 && s->out_dtype != MOE_F32) return MOE_ERR_INVALID_ARG;      // fp32 outputs have fp32 sums
     if (s->activation != MOE_ACT_NONE && s->activation != MOE_ACT_RELU && s->activation != MOE_ACT_GELU) return MOE_ERR_UNSUPPORTED;
     if (s->rows % s->k != 0) return MOE_ERR_INVALID_ARG;
     if (s->k > MOE_MAX_K) return MOE_ERR_UNSUPPORTED;
@@ -40,8 +43,9 @@ moe_status product(const moe_quant_shape* s, const void* a, const float* a_scale
     if (s->rows == 0) return MOE_OK;
     if (a == nullptr || a_scales == nullptr || w == nullptr || w_scales == nullptr || out == nullptr) return MOE_ERR_INVALID_ARG;
     if (grouped && offsets == nullptr) return MOE_ERR_INVALID_ARG;
-    if ((s->out_dtype == MOE_E4M3) != (out_scales != nullptr)) return MOE_ERR_INVALID_ARG;
-    if (!aligned(a, 16) || !aligned(w, 16) || !aligned(out, s->out_dtype == MOE_E4M3 ? 16 : element_bytes(s->out_dtype)))
+    const int type = out_type(*s);
+    if ((type == MOE_E4M3) != (out_scales != nullptr)) return MOE_ERR_INVALID_ARG;
+    if (!aligned(a, 16) || !aligned(w, 16) || !aligned(out, type == MOE_E4M3 ? 16 : element_bytes(type)))
         return MOE_ERR_INVALID_ARG;
     if (!aligned(a_scales, 4) || !aligned(w_scales, 4) || !aligned(bias, 4) || !aligned(out_scales, 4) || !aligned(perm, 4) ||
         !aligned(offsets, 4))
@@ -49,7 +53,8 @@ moe_status product(const moe_quant_shape* s, const void* a, const float* a_scale
     if (ws == nullptr || !aligned(ws, 256) || ws_bytes < quant_product_workspace(*s)) return MOE_ERR_WORKSPACE;
     if (ensure_ready() != hipSuccess) return MOE_ERR_HIP;
     const QuantArgs args{static_cast<const uint8_t*>(a), a_scales, perm, offsets, mask, static_cast<const uint8_t*>(w), w_scales, bias,
-                         out, out_scales, s->rows, s->N, s->K, s->E, perm != nullptr ? s->k : 1, s->activation, s->out_dtype};
+                         out, out_scales, s->rows, s->N, s->K, s->E, perm != nullptr ? s->k : 1, s->activation, type,
+                         s->out_dtype != type};
     return launch_quant_product(args, ws, static_cast<hipStream_t>(stream)) == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

@@ -42,13 +42,11 @@ __device__ __forceinline__ Widened widen(const i32x8& codes) {
 // which columns they are does not matter as long as both operands agree (moe.h: 64 h + 16 (l / 16), h = 0, 1).  Result i of lane l: weight
 // row 4 (l / 16) + i, token row l % 16.
 //
-// Which matrix units: those for 8-bit operands (v_mfma_f32_16x16x128_f8f6f4) take twice the products per cycle and need no widened codes,
-// but add products in groups of eight neighbours, cut at 2^-13 of the power of two of the group's largest; the groups' sums are fp32.
-// Measured: 1.5e-5 of the rms of a sum of 128 products of normal values, 5e-5 where one column of a block is 50 times the others, which is a
-// hundredth of half a step of bf16 and less than a thousandth of one of e4m3.  So outputs of these types use them, and every block's sum is
-// added to the others in fp32: 16384 x 8192 x 2048 (GeLU, e4m3) 556 -> 400 us, 1501 x 768 x 3072 (bf16) 24.4 -> 14.6.  fp32 outputs, and the
-// parts of a cut contraction, which are fp32, use the bf16 units, whose sums of widened codes are exact to 1e-8 of the rms.
-template <int OUT> constexpr bool kEightBitUnits = OUT == kOutBf16 || OUT == kOutE4m3;
+// Which matrix units (EIGHT): those for 8-bit operands (v_mfma_f32_16x16x128_f8f6f4) take twice the products per cycle and need no widened
+// codes, but add products in groups of eight neighbours, cut at 2^-13 of the power of two of the group's largest; the groups' sums are fp32.
+// Measured: 1.5e-5 of the rms of a sum of 128 products of normal values, 5e-5 where one column of a block is 50 times the others, and where
+// large products cancel, all of what they leave.  The bf16 units' sums of widened codes are exact to 1e-8 of the rms.  So the bf16 units are
+// used, and the 8-bit ones where the caller asks for them (MOE_QUANT_UNIT_SUMS); the parts of a cut contraction are fp32 sums either way.
 __device__ __forceinline__ f32x4 multiply_codes(const i32x8& w, const i32x8& x) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);     // e4m3 both, scales of one
 }
@@ -439,7 +437,7 @@ __device__ __forceinline__ int list_experts(const QuantArgs& a, int max_rows, ui
 // OUT = kOutParts: the contraction is cut into `split` parts, whose sums go to a.out as [split][rows][pitch of N] fp32.
 constexpr int kOutParts = 3;
 
-template <int OUT, int NF>
+template <int OUT, int NF, bool EIGHT>
 __device__ __forceinline__ void stream_units(const QuantArgs& a, int tiles, int parts_wanted, int b, unsigned char* smem) {
     using S = Streams<NF>;
     constexpr int kStages = S::kStages, kStage = S::kStage;
@@ -595,7 +593,7 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int tiles, int 
                 }
                 copy_next();
                 f32x4 p[NF][TF];
-                if constexpr (kEightBitUnits<OUT>) {
+                if constexpr (EIGHT) {
 #pragma unroll
                     for (int tf = 0; tf < TF; ++tf)
 #pragma unroll
@@ -677,12 +675,12 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, int tiles, int 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
 }
 
-template <int OUT>
+template <int OUT, bool EIGHT>
 __global__ __launch_bounds__(kStreamWaves * 64) void quant_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + Streams<1>::kList);
     const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
-    stream_units<OUT, 1>(a, tiles, parts_wanted, blockIdx.x, smem);
+    stream_units<OUT, 1, EIGHT>(a, tiles, parts_wanted, blockIdx.x, smem);
 }
 
 // Adds up the parts of a split contraction, in their order, and finishes the rows.  A block of threads per row and 8 groups of 128
@@ -768,10 +766,9 @@ struct Tiles {
     static_assert(kLdsBytes <= 160 * 1024, "fits a CU");
 };
 
-template <int OUT, int RMAX>
+template <int OUT, int RMAX, bool EIGHT>
 __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, unsigned char* smem) {
     using T = Tiles<RMAX>;
-    constexpr bool EIGHT = kEightBitUnits<OUT>;
     constexpr int kStages = T::kStages, kStageW = T::kStageW, kStageS = T::kStageS, kStage = T::kStage, tile_rows = T::kRows;
     uint32_t* mosts = reinterpret_cast<uint32_t*>(smem + T::kMost);           // [2][rows]
     int4* counts = reinterpret_cast<int4*>(smem + T::kStarts);
@@ -1142,10 +1139,10 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
 
 // Both kinds of units of a grouped product as one kernel, the tiles first: where one kind does not occur, a launch of its own would
 // cost 4 to 5 us all the same.  The blocks that have a tile more are the last ones to get a run of streamed units.
-template <int OUT, int RMAX>
+template <int OUT, int RMAX, bool EIGHT>
 __global__ __launch_bounds__(kTileWaves * 64) void quant_product_kernel(const QuantArgs a, int tiled_min_rows) {
     extern __shared__ __align__(16) unsigned char smem[];
-    tile_units<OUT, RMAX>(a, tiled_min_rows, smem);
+    tile_units<OUT, RMAX, EIGHT>(a, tiled_min_rows, smem);
     if (a.offsets == nullptr) return;
     __syncthreads();
     static_assert(Streams<1>::kList >= Streams<2>::kList, "the list lies behind both rings");
@@ -1154,8 +1151,8 @@ __global__ __launch_bounds__(kTileWaves * 64) void quant_product_kernel(const Qu
     const int b = gridDim.x - 1 - blockIdx.x;
     // Units of 256 columns widen each row fragment for twice the columns; but where those of 128 are at most one per block they use
     // more of the CUs.
-    if (tiles * quant_blocks(a.N) > static_cast<int>(gridDim.x)) stream_units<OUT, 2>(a, tiles, 1, b, smem);
-    else stream_units<OUT, 1>(a, tiles, 1, b, smem);
+    if (tiles * quant_blocks(a.N) > static_cast<int>(gridDim.x)) stream_units<OUT, 2, EIGHT>(a, tiles, 1, b, smem);
+    else stream_units<OUT, 1, EIGHT>(a, tiles, 1, b, smem);
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
@@ -1199,12 +1196,12 @@ static int tile_fragments(int rows, int N, size_t operand_bytes) {
 template <int RMAX>
 constexpr int kProductLds = Tiles<RMAX>::kLdsBytes > Streams<1>::kLdsBytes ? Tiles<RMAX>::kLdsBytes : Streams<1>::kLdsBytes;
 
-template <int OUT, int RMAX>
+template <int OUT, int RMAX, bool EIGHT>
 static void launch_tiles(const QuantArgs& a, int grid, hipStream_t stream) {
-    quant_product_kernel<OUT, RMAX><<<dim3(grid), dim3(kTileWaves * 64), kProductLds<RMAX>, stream>>>(a, kTiledMinRows);
+    quant_product_kernel<OUT, RMAX, EIGHT><<<dim3(grid), dim3(kTileWaves * 64), kProductLds<RMAX>, stream>>>(a, kTiledMinRows);
 }
 
-template <int OUT>
+template <int OUT, bool EIGHT>
 static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
     const int cus = device_cu_count();
     const dim3 grid(cus), threads(kStreamWaves * 64);
@@ -1212,43 +1209,40 @@ static hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
     if (split > 1) {
         QuantArgs parts = a;
         parts.out = ws;
-        quant_stream_kernel<kOutParts><<<grid, threads, Streams<1>::kLdsBytes, stream>>>(parts, a.rows, split);
+        quant_stream_kernel<kOutParts, false><<<grid, threads, Streams<1>::kLdsBytes, stream>>>(parts, a.rows, split);
         quant_join_kernel<OUT><<<dim3(a.rows, (quant_blocks(a.N) + 7) / 8), dim3(256), 0, stream>>>(a, static_cast<const float*>(ws), split);
         return hipGetLastError();
     }
     if (a.rows >= kTiledMinRows) {
         const int r = tile_fragments(a.rows, a.N, a.rows / a.k * quant_pitch(a.K));
-        if (r == 4) launch_tiles<OUT, 4>(a, cus, stream);
-        else if (r == 2) launch_tiles<OUT, 2>(a, cus, stream);
-        else launch_tiles<OUT, 1>(a, cus, stream);
+        if (r == 4) launch_tiles<OUT, 4, EIGHT>(a, cus, stream);
+        else if (r == 2) launch_tiles<OUT, 2, EIGHT>(a, cus, stream);
+        else launch_tiles<OUT, 1, EIGHT>(a, cus, stream);
     } else {
-        quant_stream_kernel<OUT><<<grid, threads, Streams<1>::kLdsBytes, stream>>>(a, a.rows, 1);
+        quant_stream_kernel<OUT, EIGHT><<<grid, threads, Streams<1>::kLdsBytes, stream>>>(a, a.rows, 1);
     }
     return hipGetLastError();
 }
 
+static hipError_t allow_lds(const void* kernel, int bytes) {
+    return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+}
+template <int OUT, bool EIGHT>
+static hipError_t configure_out() {
+    hipError_t e;
+    if ((e = allow_lds(reinterpret_cast<const void*>(quant_product_kernel<OUT, 4, EIGHT>), kProductLds<4>)) != hipSuccess) return e;
+    if ((e = allow_lds(reinterpret_cast<const void*>(quant_product_kernel<OUT, 2, EIGHT>), kProductLds<2>)) != hipSuccess) return e;
+    if ((e = allow_lds(reinterpret_cast<const void*>(quant_product_kernel<OUT, 1, EIGHT>), kProductLds<1>)) != hipSuccess) return e;
+    return allow_lds(reinterpret_cast<const void*>(quant_stream_kernel<OUT, EIGHT>), Streams<1>::kLdsBytes);
+}
 hipError_t configure_quant_kernels() {
-    const struct {
-        const void* kernel;
-        int lds;
-    } all[] = {{reinterpret_cast<const void*>(quant_product_kernel<kOutF32, 4>), kProductLds<4>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutF32, 2>), kProductLds<2>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutF32, 1>), kProductLds<1>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutBf16, 4>), kProductLds<4>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutBf16, 2>), kProductLds<2>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutBf16, 1>), kProductLds<1>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 4>), kProductLds<4>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 2>), kProductLds<2>},
-               {reinterpret_cast<const void*>(quant_product_kernel<kOutE4m3, 1>), kProductLds<1>},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutF32>), Streams<1>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutBf16>), Streams<1>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutE4m3>), Streams<1>::kLdsBytes},
-               {reinterpret_cast<const void*>(quant_stream_kernel<kOutParts>), Streams<1>::kLdsBytes}};
-    for (const auto& k : all) {
-        const hipError_t e = hipFuncSetAttribute(k.kernel, hipFuncAttributeMaxDynamicSharedMemorySize, k.lds);
-        if (e != hipSuccess) return e;
-    }
-    return hipSuccess;
+    hipError_t e;
+    if ((e = configure_out<kOutF32, false>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutBf16, false>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutBf16, true>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutE4m3, false>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutE4m3, true>()) != hipSuccess) return e;
+    return allow_lds(reinterpret_cast<const void*>(quant_stream_kernel<kOutParts, false>), Streams<1>::kLdsBytes);
 }
 
 // Weights that do not fit the L2s (8 x 4 MiB) are gone before the next call reads them: streamed units then read them as what is read once,
@@ -1260,9 +1254,9 @@ constexpr size_t kCachedWeights = size_t{32} << 20;
 hipError_t launch_quant_product(const QuantArgs& args, void* ws, hipStream_t stream) {
     QuantArgs a = args;
     a.once = a.E * quant_matrix_bytes(a.N, a.K) > kCachedWeights;
-    if (a.out_dtype == MOE_F32) return launch_out<kOutF32>(a, ws, stream);
-    if (a.out_dtype == MOE_BF16) return launch_out<kOutBf16>(a, ws, stream);
-    return launch_out<kOutE4m3>(a, ws, stream);
+    if (a.out_dtype == MOE_F32) return launch_out<kOutF32, false>(a, ws, stream);
+    if (a.out_dtype == MOE_BF16) return a.unit_sums ? launch_out<kOutBf16, true>(a, ws, stream) : launch_out<kOutBf16, false>(a, ws, stream);
+    return a.unit_sums ? launch_out<kOutE4m3, true>(a, ws, stream) : launch_out<kOutE4m3, false>(a, ws, stream);
 }
 
 }  // namespace moe

@@ -6,6 +6,9 @@ and weights, combine.  `QuantDenseBlock`: the same for the dense layers between 
     block = QuantMoEBlock(T, d_model, d_ff, E, k, w1, w2, w_gate, norm_weight)      # w1 [E, d_ff, d_model], w2 [E, d_model, d_ff]
     y, stream = block.forward(x, residual)     # stream = x + residual continues; y is the next block's x
 
+Sums are fp32; with sums="units" those of bf16 and e4m3 outputs come from the matrix units for 8-bit operands, which are faster for many
+tokens and less exact (moe.h, MOE_QUANT_UNIT_SUMS).
+
 Both products of a step of T tokens use workspaces that are made once; a block of another T shares the weights through `resized`.
 """
 from __future__ import annotations
@@ -74,8 +77,8 @@ class _Block:
 
 class QuantMoEBlock(_Block):
     def __init__(self, T, d_model, d_ff, E, k, w1, w2, w_gate, norm_weight=None, *, w1_scales=None, w2_scales=None, gate_bias=None, b1=None,
-                 b2=None, activation="relu", renormalize=True, eps=1e-6):
-        self.T, self.d_model, self.d_ff, self.E, self.k = T, d_model, d_ff, E, k
+                 b2=None, activation="relu", renormalize=True, eps=1e-6, sums="f32"):
+        self.T, self.d_model, self.d_ff, self.E, self.k, self.sums = T, d_model, d_ff, E, k, sums
         self.device, self.eps, self.activation, self.renormalize = w1.device, eps, activation, renormalize
         self.w1, self.w2 = QuantWeights(w1, w1_scales), QuantWeights(w2, w2_scales)
         if (self.w1.E, self.w1.N, self.w1.K) != (E, d_ff, d_model) or (self.w2.E, self.w2.N, self.w2.K) != (E, d_model, d_ff):
@@ -88,7 +91,7 @@ class QuantMoEBlock(_Block):
         A = T * k
         self._norm_buffers(norm_out=True)
         self.layer = make_shape(T, self.d_model, self.d_ff, E, k, "bf16", self.renormalize)
-        self.first = make_quant_shape(A, self.d_ff, self.d_model, E, k, self.activation, "e4m3")
+        self.first = make_quant_shape(A, self.d_ff, self.d_model, E, k, self.activation, "e4m3", self.sums)
         self.second = make_quant_shape(A, self.d_model, self.d_ff, E, 1, "none", "f32")
         i32 = torch.int32
         self.topk_idx = torch.empty((T, k), dtype=i32, device=dev)
@@ -120,8 +123,8 @@ class QuantMoEBlock(_Block):
 
 class QuantDenseBlock(_Block):
     def __init__(self, T, d_model, d_ff, w1, w2, norm_weight=None, *, w1_scales=None, w2_scales=None, b1=None, b2=None, activation="relu",
-                 eps=1e-6):
-        self.T, self.d_model, self.d_ff = T, d_model, d_ff
+                 eps=1e-6, sums="f32"):
+        self.T, self.d_model, self.d_ff, self.sums = T, d_model, d_ff, sums
         self.device, self.eps, self.activation, self.norm_weight, self.b1, self.b2 = w1.device, eps, activation, norm_weight, b1, b2
         one = lambda t: None if t is None else t[None]
         self.w1, self.w2 = QuantWeights(w1[None], one(w1_scales)), QuantWeights(w2[None], one(w2_scales))
@@ -131,8 +134,8 @@ class QuantDenseBlock(_Block):
 
     def _buffers(self):
         self._norm_buffers(norm_out=False)
-        self.first = make_quant_shape(self.T, self.d_ff, self.d_model, 1, 1, self.activation, "e4m3")
-        self.second = make_quant_shape(self.T, self.d_model, self.d_ff, 1, 1, "none", "bf16")
+        self.first = make_quant_shape(self.T, self.d_ff, self.d_model, 1, 1, self.activation, "e4m3", self.sums)
+        self.second = make_quant_shape(self.T, self.d_model, self.d_ff, 1, 1, "none", "bf16", self.sums)
         self.h8 = _Rows(self.T, self.d_ff, self.device)
         self.ws1, self.ws2 = self._workspace(self.first), self._workspace(self.second)
 

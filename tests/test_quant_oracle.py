@@ -140,3 +140,21 @@ def test_binding_refuses_other_layouts():
     t = torch.zeros((4, 128))
     with pytest.raises(ValueError, match="CUDA"):
         moe.moe_norm_quantize(4, 128, "f32", t, None, None, 1e-6, None, None, t, t)
+
+
+def test_sums_are_the_callers_choice():
+    """fp32 unless MOE_QUANT_UNIT_SUMS is asked for, which fp32 outputs refuse."""
+    assert moe.make_quant_shape(4, 128, 128, out_dtype="e4m3").out_dtype == moe.MOE_E4M3
+    for out, value in (("bf16", moe.MOE_BF16), ("e4m3", moe.MOE_E4M3)):
+        s = moe.make_quant_shape(4, 128, 128, out_dtype=out, sums="units")
+        assert s.out_dtype == value | moe.MOE_QUANT_UNIT_SUMS
+        assert moe.moe_quant_workspace_bytes(s) == moe.moe_quant_workspace_bytes(moe.make_quant_shape(4, 128, 128, out_dtype=out)) > 0
+    s = moe.make_quant_shape(4, 128, 128, out_dtype="f32", sums="units")
+    assert moe.moe_quant_workspace_bytes(s) == 0
+    assert status("moe_quant_linear", ctypes.byref(s), FAKE, FAKE, FAKE, FAKE, None, FAKE, None, FAKE, 1 << 30, None) == moe.MOE_ERR_INVALID_ARG
+    # a quantised output still needs its scales, a bf16 one takes none
+    for out, scales in (("e4m3", None), ("bf16", FAKE)):
+        s = moe.make_quant_shape(4, 128, 128, out_dtype=out, sums="units")
+        assert status("moe_quant_linear", ctypes.byref(s), FAKE, FAKE, FAKE, FAKE, None, FAKE, scales, FAKE, 1 << 30, None) == moe.MOE_ERR_INVALID_ARG
+    with pytest.raises(KeyError):
+        moe.make_quant_shape(4, 128, 128, sums="bf16")
