@@ -325,9 +325,9 @@ moe_status moe_layer_forward_noalloc(const moe_shape* shape, const void* x, cons
  *
  * Quantised rows [R, C]: e4m3 codes in rows of moe_quant_pitch(C) bytes (C rounded up to 128; the codes past C are zero) and
  * fp32 scales [R, ceil(C / 128)]; value (r, c) is code(r, c) * scale(r, c / 128).  As these calls write them, a block of 128
- * values (a row's last block may be shorter) has scale = max(max |v| / 448, 2^-126) and code = v / scale rounded to the nearest
- * e4m3 value, ties to even; a block that holds a NaN or an infinity has a NaN for its scale and NaN codes, so that it is NaN
- * throughout.  The products take any scales.
+ * values (a row's last block may be shorter) has scale = max(max |v| / 448, 2^-126) and code = v / scale, rounded to fp32 and from there
+ * to the nearest e4m3 value, ties to even (moe_norm_quantize rounds once, from 64 bits); a block that holds a NaN or an infinity has a
+ * NaN for its scale and NaN codes, so that it is NaN throughout.  The products take any scales.
  * Quantised weights of E matrices [N, K] ("out-features x in-features"): scales [E, ceil(N / 128), ceil(K / 128)], one for every
  * 128 x 128 block, and the codes in the products' layout, made once by moe_quantize_weights.
  * Codes and packed weights are 16-byte aligned, other pointers to the size of their elements.

@@ -36,6 +36,20 @@ __device__ __forceinline__ float block_scale(uint32_t most) {
     return fmaxf(__uint_as_float(most) / kE4m3Max, kMinScale);
 }
 
+// v / scale of a block's values as fp32 division rounds it, which a product with the reciprocal does not (of the middles between two codes it
+// puts one in eight on a side): the product, corrected by its remainder, which is exact.  Tiny scales are taken up first, so that no remainder
+// falls below fp32's range.  Three operations more per value than the product: 16384 x 8192 x 2048 with GeLU 554 -> 579 us.
+struct BlockQuotient {
+    float up, by, inv;
+    __device__ __forceinline__ explicit BlockQuotient(float scale)
+        : up(scale < 0x1p-64f ? 0x1p64f : 1.f), by(scale * up), inv(1.f / by) {}
+    __device__ __forceinline__ float operator()(float v) const {
+        v *= up;
+        const float q = v * inv;
+        return fmaf(fmaf(-q, by, v), inv, q);
+    }
+};
+
 // Maximum over the 16 lanes of a row of lanes, in every one of them (DPP rotations within the row).
 __device__ __forceinline__ uint32_t row16_max(uint32_t v) {
     v = max(v, static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x128, 0xF, 0xF, false)));

@@ -321,13 +321,14 @@ __device__ __forceinline__ void store_codes(const QuantArgs& a, int n0, int row0
 #pragma unroll
     for (int tf = 0; tf < TF; ++tf) {
         const size_t row = static_cast<size_t>(row0 + tf * STRIDE + r);
-        const float scale = block_scale(most[tf]), inv = __builtin_amdgcn_rcpf(scale);
+        const float scale = block_scale(most[tf]);
+        const BlockQuotient of(scale);
         uint32_t codes[NF];
 #pragma unroll
         for (int nf = 0; nf < NF; ++nf) {
             const int n = n0 + nf * 16 + g * 4;
             const f32x4 v = acc[nf][tf];
-            codes[nf] = pack_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            codes[nf] = pack_e4m3x4(of(v[0]), of(v[1]), of(v[2]), of(v[3]));
             if (n + 4 > a.N) codes[nf] = n >= a.N ? 0u : codes[nf] & (0xffffffffu >> (8 * (n + 4 - a.N)));     // zeros past the end
         }
         if constexpr (NF == 4) gather_columns(codes);
@@ -721,9 +722,10 @@ __global__ __launch_bounds__(256) void quant_join_kernel(const QuantArgs a, cons
     if constexpr (OUT == kOutE4m3) {
         most = row16_max(most);
         most = max(most, static_cast<uint32_t>(__shfl_xor(static_cast<int>(most), 16, 64)));       // 32 lanes are a block of 128
-        const float scale = block_scale(most), inv = 1.f / scale;
+        const float scale = block_scale(most);
+        const BlockQuotient of(scale);
         if (n0 < static_cast<int>(pitch)) {
-            uint32_t codes = pack_e4m3x4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            uint32_t codes = pack_e4m3x4(of(v[0]), of(v[1]), of(v[2]), of(v[3]));
             if (n0 + 4 > a.N) codes = n0 >= a.N ? 0u : codes & (0xffffffffu >> (8 * (n0 + 4 - a.N)));
             *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(a.out) + row * pitch + n0) = codes;
             if ((lane & 31) == 0) a.out_scales[static_cast<size_t>(row) * quant_blocks(a.N) + n0 / kQuantBlock] = scale;

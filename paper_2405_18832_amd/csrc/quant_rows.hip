@@ -336,14 +336,15 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const ST* __restr
         if ((threadIdx.x & 63) == 0) all[threadIdx.x >> 6] = most;
         __syncthreads();
         most = max(max(all[0], all[1]), max(all[2], all[3]));
-        const float scale = block_scale(most), inv = 1.f / scale;
+        const float scale = block_scale(most);
+        const BlockQuotient of(scale);
         if (threadIdx.x == 0) scales[(static_cast<size_t>(e) * nblocks + nb) * kblocks + kb] = scale;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const float* u = v[i][q >> 1] + 4 * (q & 1);
-                codes[i][q] = pack_e4m3x4(u[0] * inv, u[1] * inv, u[2] * inv, u[3] * inv);
+                codes[i][q] = pack_e4m3x4(of(u[0]), of(u[1]), of(u[2]), of(u[3]));
                 // columns and rows past the end stay zero in a block whose scale is NaN
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
