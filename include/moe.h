@@ -384,7 +384,7 @@ typedef struct {
  */
 #define MOE_QUANT_UNIT_SUMS 0x100
 
-/* Bytes of workspace of the two calls below (0 on a shape that they refuse). */
+/* Bytes of workspace of the two calls below (0 on a shape that they refuse; rows == 0, a no-op, is none). */
 size_t moe_quant_workspace_bytes(const moe_quant_shape* shape);
 
 /*

@@ -1166,7 +1166,7 @@ constexpr int kTiledMinRows = 65;
 // (1 x 2048 x 8192); but 128 units 13.3 -> 14.5 us with two (the experts of one token, 8192 x 2048).
 // A grouped call's number of experts with rows is not known here; a row each is taken, the most it can be.
 static int stream_split(int rows, int N, int K, int E) {
-    if (rows >= kTiledMinRows) return 1;
+    if (rows == 0 || rows >= kTiledMinRows) return 1;
     const int units = std::min(rows, E) * quant_blocks(N);
     return units <= 96 ? std::max(1, std::min(256 / units, quant_blocks(K) / 2)) : 1;
 }

@@ -158,3 +158,13 @@ def test_sums_are_the_callers_choice():
         assert status("moe_quant_linear", ctypes.byref(s), FAKE, FAKE, FAKE, FAKE, None, FAKE, scales, FAKE, 1 << 30, None) == moe.MOE_ERR_INVALID_ARG
     with pytest.raises(KeyError):
         moe.make_quant_shape(4, 128, 128, sums="bf16")
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16", "e4m3"])
+@pytest.mark.parametrize("E", [1, 2, 1024])
+@pytest.mark.parametrize("N,K", [(1, 1), (256, 256), (2048, 8192)])
+def test_workspace_of_no_rows(N, K, E, out):
+    """A call without rows is a no-op, and its size query answers."""
+    s = moe.make_quant_shape(0, N, K, E, 1, "none", out)
+    assert moe.moe_quant_workspace_bytes(s) == 256
+    assert status("moe_quant_expert_linear", ctypes.byref(s), None, None, None, None, None, None, None, None, None, None, None, 0, None) == moe.MOE_OK
