@@ -151,7 +151,7 @@ template <typename ST, int WPR, int NV, bool WHOLE>
 __global__ __launch_bounds__(kNormWaves * 64) void norm_quantize_kernel(const NormArgs a) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int part = wave % WPR;
-    const int row = blockIdx.x * (kNormWaves / WPR) + wave / WPR;
+    const int row = (blockIdx.y * gridDim.x + blockIdx.x) * (kNormWaves / WPR) + wave / WPR;
     const bool live = row < a.rows;                         // the block meets at a barrier below
     const int d = a.d;
     const size_t at = static_cast<size_t>(live ? row : 0) * d;
@@ -258,9 +258,11 @@ template <typename ST, bool WHOLE>
 static hipError_t launch_norm(const NormArgs& a, hipStream_t stream) {
     const int chunks = static_cast<int>((quant_pitch(a.d) + kNormValues - 1) / kNormValues);
     const dim3 block(kNormWaves * 64);
+    // a launch counts at most 2^32 - 1 threads in one direction: 2^24 blocks are one too many
+    constexpr int kAcross = 1 << 22;
     auto go = [&](auto kernel, int wpr) {
-        const int per_block = kNormWaves / wpr;
-        kernel<<<dim3((a.rows + per_block - 1) / per_block), block, 0, stream>>>(a);
+        const int per_block = kNormWaves / wpr, blocks = (a.rows + per_block - 1) / per_block;
+        kernel<<<dim3(blocks < kAcross ? blocks : kAcross, (blocks + kAcross - 1) / kAcross), block, 0, stream>>>(a);
     };
     // as many wavefronts per row as it has chunks
     if (chunks == 1) go(norm_quantize_kernel<ST, 1, 1, WHOLE>, 1);
