@@ -75,7 +75,6 @@ moe_status moe_quantize_weights(int32_t E, int32_t N, int32_t K, int32_t src_dty
     if (src_dtype != MOE_F32 && src_dtype != MOE_BF16 && src_dtype != MOE_E4M3) return MOE_ERR_INVALID_ARG;
     if (src == nullptr || dst == nullptr || src == dst || (src_dtype != MOE_E4M3 && scales == nullptr)) return MOE_ERR_INVALID_ARG;
     if (!aligned(dst, 16) || !aligned(src, element_bytes(src_dtype)) || !aligned(scales, 4)) return MOE_ERR_INVALID_ARG;
-    if (quant_blocks(N) > 65535) return MOE_ERR_UNSUPPORTED;                // blocks of a grid in its second direction
     if (ensure_ready() != hipSuccess) return MOE_ERR_HIP;
     return launch_quantize_weights(E, N, K, src_dtype, src, static_cast<uint8_t*>(dst), scales, static_cast<hipStream_t>(stream)) ==
                    hipSuccess

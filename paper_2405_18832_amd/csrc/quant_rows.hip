@@ -1,4 +1,5 @@
 // Quantised rows and weights: the RMS norm in front of a layer with the residual's addition, and the weights' layout.
+#include <algorithm>
 #include <type_traits>
 
 #include "quant.hpp"
@@ -291,9 +292,11 @@ typedef __attribute__((ext_vector_type(4), aligned(1))) uint32_t any_codes16;
 
 template <typename ST>      // float, uint16_t (bf16) or uint8_t (codes)
 __global__ __launch_bounds__(256) void quantize_weights_kernel(const ST* __restrict__ src, uint8_t* __restrict__ dst,
-                                                               float* __restrict__ scales, int N, int K) {
-    const int kb = blockIdx.x, nb = blockIdx.y, e = blockIdx.z;
-    const int kblocks = gridDim.x, nblocks = gridDim.y;
+                                                               float* __restrict__ scales, int N, int K, int parts) {
+    // the row blocks of a matrix may need several of the grid's second direction
+    const int kb = blockIdx.x, e = blockIdx.z / parts, nb = (blockIdx.z - e * parts) * gridDim.y + blockIdx.y;
+    const int kblocks = gridDim.x, nblocks = quant_blocks(N);
+    if (nb >= nblocks) return;
     const int piece = threadIdx.x & 7, r0 = threadIdx.x >> 3;
     const int c0 = kb * kQuantBlock + piece * 16;
     auto row_of = [&](int i) { return nb * kQuantBlock + r0 + 32 * i; };
@@ -363,10 +366,14 @@ __global__ __launch_bounds__(256) void quantize_weights_kernel(const ST* __restr
 }
 
 hipError_t launch_quantize_weights(int E, int N, int K, int src_dtype, const void* src, uint8_t* dst, float* scales, hipStream_t stream) {
-    const dim3 grid(quant_blocks(K), quant_blocks(N), E), block(256);
-    if (src_dtype == MOE_F32) quantize_weights_kernel<<<grid, block, 0, stream>>>(static_cast<const float*>(src), dst, scales, N, K);
-    else if (src_dtype == MOE_BF16) quantize_weights_kernel<<<grid, block, 0, stream>>>(static_cast<const uint16_t*>(src), dst, scales, N, K);
-    else quantize_weights_kernel<<<grid, block, 0, stream>>>(static_cast<const uint8_t*>(src), dst, scales, N, K);
+    constexpr int kAcross = 32768;              // blocks of the grid's second and third direction: at most 65535
+    static_assert(MOE_MAX_E * (kMaxQuantDim / kQuantBlock / kAcross) <= 65535, "of the third");
+    const int nblocks = quant_blocks(N), parts = (nblocks + kAcross - 1) / kAcross;
+    const dim3 grid(quant_blocks(K), std::min(nblocks, kAcross), E * parts), block(256);
+    auto go = [&](auto* from) { quantize_weights_kernel<<<grid, block, 0, stream>>>(from, dst, scales, N, K, parts); };
+    if (src_dtype == MOE_F32) go(static_cast<const float*>(src));
+    else if (src_dtype == MOE_BF16) go(static_cast<const uint16_t*>(src));
+    else go(static_cast<const uint8_t*>(src));
     return hipGetLastError();
 }
 
