@@ -100,10 +100,12 @@ __device__ __forceinline__ int source_row(const QuantArgs& a, int p) {
 // a launch.  whole[e] is the number of tiles of `tile_rows` rows that the experts before e have, whole[E] that of all; `rest` lists the
 // experts with a shorter last tile, those of more than 128 rows first, then of more than 64, then the others, so that units of one length
 // are handed out together.  Returns how many of these there are.  `tmp`: four ints per wavefront.
+// Offsets that are none (0, rows, 0, rows, ...) may give every other expert all rows: the whole tiles end at as many as the rows have, which
+// keeps their number times the column groups within 32 bits.
 template <int THREADS>
 __device__ __forceinline__ int count_tiles(const QuantArgs& a, int tile_rows, int min_rows, int32_t* whole, uint16_t* rest, int4* tmp) {
     constexpr int W = THREADS / 64;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, most = a.rows / tile_rows;
     int4 before = {0, 0, 0, 0};            // whole tiles, and last tiles by length
     int kind_base[3] = {0, 0, 0};
     // the lengths' totals are needed before the first expert's place is known: first pass counts, second one places
@@ -128,11 +130,11 @@ __device__ __forceinline__ int count_tiles(const QuantArgs& a, int tile_rows, in
             int4 mine = before;
             for (int w = 0; w < W; ++w) {
                 const int4 t = tmp[w];
-                if (w < wave) mine = int4{mine.x + t.x, mine.y + t.y, mine.z + t.z, mine.w + t.w};
-                before = int4{before.x + t.x, before.y + t.y, before.z + t.z, before.w + t.w};
+                if (w < wave) mine = int4{min(mine.x + t.x, most), mine.y + t.y, mine.z + t.z, mine.w + t.w};
+                before = int4{min(before.x + t.x, most), before.y + t.y, before.z + t.z, before.w + t.w};
             }
             if (pass == 1) {
-                if (e < a.E) whole[e] = mine.x + incl - n;
+                if (e < a.E) whole[e] = min(mine.x + incl - n, most);
                 const uint64_t below = (1ull << lane) - 1;
                 const int at = kind == 0 ? mine.y + __popcll(k0 & below)
                              : kind == 1 ? kind_base[1] + mine.z + __popcll(k1 & below)
