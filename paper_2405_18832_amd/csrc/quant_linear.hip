@@ -396,8 +396,8 @@ __device__ __forceinline__ int row_operand_other(int at) { return at & 64 ? -64 
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
 // Unit: an expert's rows, at most 64, x 128 NF columns, by 8 wavefronts of 16 NF columns each, a block of 128 columns of the contraction
-// per step.  Bound by memory (49 experts of one to three rows, 2048 x 8192: 136 to 140 us = 6.1 to 6.3 TB/s; 64 experts of 32 rows, 3072 x
-// 768: 35 us = 4.3 TB/s, 3 of them for the launch), so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
+// per step.  Bound by memory (49 experts of one to three rows, 2048 x 8192: 131 to 140 us = 6.1 to 6.5 TB/s; 64 experts of 32 rows, 3072 x
+// 768, e4m3 out: 39 us = 3.9 TB/s, 34 with the 8-bit units, 3 of them for the launch), so what matters is that copies never stop: weights (16 NF KiB a step), rows and scales go to LDS directly,
 // through a ring of stages that runs on across units.  A block's units follow each other in one expert, where nothing needs to be looked
 // up (a load that the compiler sees would make it wait for every copy in flight).
 constexpr int kStreamRows = 64, kStreamWaves = 8;
@@ -752,13 +752,13 @@ __global__ __launch_bounds__(256) void quant_join_kernel(const QuantArgs a, cons
 //   scales   of the rows, and the weights' (one for the unit's 128 columns)
 // Wavefront (wm, wn) of the 4 x 2 multiplies row fragments wm, wm + 4, ... (R of them) and the columns 64 wn ... 64 wn + 63.
 //
-// What bounds it, with the 8-bit units (16384 x 8192 x 8192, bf16 out: 1054 us = 2090 TFLOP/s; x 2048: 295 us = 1860; a library product
-// with one scale per operand, 16384 x 8192 x 2048: 254 us): the power limit, under which the clock falls to 1.4 to 1.8 GHz, and the copies.  A
-// copy of this kernel without the copies took 771 us, without the LDS reads 1045, with neither 698, without the multiply-adds 1058; copying
-// one stage over and over 1043, so that it is not the distance to the memory.  Units of 256 x 256, which copy a third less per product, took 1064
-// us, and 349 instead of 307 for 2048 columns of contraction: the next unit's copies have half the time, twice the sums are finished at once
-// and registers run out there.  Finishing and storing is 37 us of the 295, GeLU 45 more.  With the bf16 units (fp32 out, 16384 x 2048 x 8192:
-// 460 us = 1200 TFLOP/s) the vector unit is the bound, which widens 128 x 64 codes per matrix unit and step.
+// What bounds it: with the bf16 units the vector unit, which widens 128 x 64 codes per matrix unit and step (16384 x 8192 x 8192, bf16 out: 1776
+// us = 1240 TFLOP/s; x 2048: 483 us = 1140; with GeLU to e4m3 568; 16384 x 2048 x 8192, fp32 out: 460 us = 1200).  With the 8-bit units (1050 us =
+// 2090 TFLOP/s; 296 = 1860; 363; a library product with one scale per operand, 16384 x 8192 x 2048: 254 us) the power limit, under which the
+// clock falls to 1.4 to 1.8 GHz, and the copies: of 1054 us a copy of this kernel without the copies took 771, without the LDS reads 1045, with
+// neither 698, without the multiply-adds 1058, copying one stage over and over 1043, so that it is not the distance to the memory.  Units of
+// 256 x 256, which copy a third less per product, took 1064 us where this kernel took 1095 on the same card, but 349 against 307 for 2048
+// columns of contraction: the next unit's copies have half the time, twice the sums are finished at once and registers run out there.
 constexpr int kTileWaves = 8;
 template <int RMAX>
 struct Tiles {
@@ -1142,7 +1142,8 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
 }
 
 // Both kinds of units of a grouped product as one kernel, the tiles first: where one kind does not occur, a launch of its own would
-// cost 4 to 5 us all the same.  The blocks that have a tile more are the last ones to get a run of streamed units.
+// cost 4 to 5 us all the same.  Streamed units are dealt from the last block number down, evenly over the XCDs; the blocks that have a tile more
+// than others are whole XCDs, so that some of those get streamed units too while others have neither (128 of each: 64 blocks have both).
 template <int OUT, int RMAX, bool EIGHT>
 __global__ __launch_bounds__(kTileWaves * 64) void quant_product_kernel(const QuantArgs a, int tiled_min_rows) {
     extern __shared__ __align__(16) unsigned char smem[];
@@ -1165,7 +1166,8 @@ constexpr int kTiledMinRows = 65;
 
 // Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave most CUs without one.
 // It costs a second launch: one to four parts of 64 units 14.7 -> 12.4 us (32 x 8192 x 2048), of 16 units to sixteen 13.7 -> 11.3 us
-// (1 x 2048 x 8192); but 128 units 13.3 -> 14.5 us with two (the experts of one token, 8192 x 2048).
+// (1 x 2048 x 8192); but 128 units 13.3 -> 14.5 us with two (the experts of one token, 8192 x 2048).  Tiles are not cut, however few: 65 rows x
+// 2048 x 8192 take 51 us (26 with the 8-bit units), 64 rows 16.
 // A grouped call's number of experts with rows is not known here; a row each is taken, the most it can be.
 static int stream_split(int rows, int N, int K, int E) {
     if (rows == 0 || rows >= kTiledMinRows) return 1;
@@ -1183,8 +1185,8 @@ size_t quant_product_workspace(const moe_quant_shape& s) {
 // occupy more CUs.  A step of 256, 128 and 64 rows takes 1.95, 1.2 and 0.8 us on a CU with the bf16 units, 0.95, 0.7 and 0.6 with the 8-bit
 // ones; a unit of each kind has as many steps as the other, so what counts is rounds of 256 units times that.  The ratios of the first three are
 // taken for both: with each kind forced, the choice was the fastest one or within 5 % of it for each of 22 shapes of 200 to 8000 rows
-// (64, 128, 256 rows, us; bf16 out: 1501 x 768 x 3072 16.0, 21.3, 30.1; 4096 x 1024 x 4096 31.8, 26.9, 41.0; 2048 x 8192 x 2048 65.4,
-// 53.0, 45.5; fp32 out: 25.4, 33.4, 46.9; 54.1, 41.7, 64.5; 109, 84, 74).  A grouped call's last tiles are not known here and left out.
+// (64, 128, 256 rows, us; by the 8-bit units, bf16 out: 1501 x 768 x 3072 16.0, 21.3, 30.1; 4096 x 1024 x 4096 31.8, 26.9, 41.0; 2048 x 8192 x 2048 65.4,
+// 53.0, 45.5; by the bf16 units, fp32 out: 25.4, 33.4, 46.9; 54.1, 41.7, 64.5; 109, 84, 74).  A grouped call's last tiles are not known here and left out.
 // Tiles of 256 rows address the rows by 32-bit offsets.
 static int tile_fragments(int rows, int N, size_t operand_bytes) {
     auto cost = [&](int r, float step) {
@@ -1249,10 +1251,11 @@ hipError_t configure_quant_kernels() {
     return allow_lds(reinterpret_cast<const void*>(quant_stream_kernel<kOutParts, false>), Streams<1>::kLdsBytes);
 }
 
-// Weights that do not fit the L2s (8 x 4 MiB) are gone before the next call reads them: streamed units then read them as what is read once,
-// and leave the caches to the rows (Switch-base pair with its combine 81.6 -> 77.0 us, 16384 skewed tokens 1037 -> 1020; 32 tokens of 128
-// experts, 2048 x 8192, where runs of one build differ by 10 %, 136 to 150 -> 133 to 140).  A
-// matrix that fits may still be there (32 x 8192 x 2048, 17 MB, called again and again: 10.8 us, read as once 12.0).
+// Weights that do not fit the L2s (8 x 4 MiB) are gone before the next call reads them, or have pushed out the rows: streamed units then read
+// them as what is read once.  Kept and read once, us, the same weights again and others in turn (bf16 out): 32 rows x 8192 x 2048, 17 MB, 11.1 and
+// 11.1, 12.4 and 12.3 (e4m3 out, again: 10.9 and 12.1); 26 MB 12.9 and 13.2, 14.5 and 14.2; 50 MB 16.4 and 16.5, 17.3 and 17.7; 67 MB 19.5 and 18.9,
+// 23.3 and 21.6; 134 MB 38.2 and 37.7, 39.2 and 38.0; 400 MB 110 and 106 both ways.  Grouped: 40 experts, 42 MB, 11.2 and 10.2, 12.5 and 11.7; 64 experts
+// of 32 rows, 151 MB, 29.2 and 32.6 (the memory-side cache holds them), 37.2 and 34.6; 49 of 128 experts, 2 GB of which 822 MB are read, 141 and 131.
 constexpr size_t kCachedWeights = size_t{32} << 20;
 
 hipError_t launch_quant_product(const QuantArgs& args, void* ws, hipStream_t stream) {

@@ -9,7 +9,7 @@ namespace moe {
 // ---- moe_norm_quantize ----------------------------------------------------------------------------------------------
 // One pass over the data: the row is read once (x, residual), kept in registers as fp32, its squares are summed, and sum, norm and
 // codes are written from the registers.  Bound by memory: per value 2 or 4 + 4 bytes in, 1 to 9 out; 16384 x 2048 (bf16, all outputs)
-// 57 us = 5.3 TB/s, which is what a large copy reaches; 5000 x 1024 11.6 us, of which 3 are a launch.
+// 57 us = 5.3 TB/s (a copy of 2 GiB: 4.9); 5000 x 1024 11.6 us, of which 3 are a launch.
 //
 // A lane holds chunks of 8 consecutive values, so that 16 lanes are a block of 128 (its maximum takes four DPP rotations) and a
 // wavefront covers 512 values per chunk; chunk c of a row is done by wavefront c % WPR of the row's WPR wavefronts: as many as it has chunks, up
@@ -94,16 +94,18 @@ __device__ __forceinline__ float wave_sum(float v) {
 
 // Whether v, with the rounding errors that it has from its way through fp32 (a few steps), may lie on the other side of the middle
 // between two codes than the number it stands for.  From 2^-6 on codes have 3 bits behind the leading one; below (one value in 10^4 of
-// a normal block) nothing is said.
+// a normal block, more where a few values are much larger than the others) nothing is said.
 __device__ __forceinline__ bool next_to_a_border(float v) {
     const uint32_t m = magnitude(v);
     const int32_t past = static_cast<int32_t>(m & 0xfffffu) - 0x80000;
     return m >= 0x3c800000u ? past >= -16 && past <= 16 : m != 0;
 }
 
-// The same quotients from 64 bits, for chunks in which one is next to a border (one in twenty): s w is exact there, and divided by the
+// The same quotients from 64 bits, for chunks in which one is next to a border: s w is exact there, and divided by the
 // block's largest the row's rho goes out.  Each is left as the fp32 number with an odd last bit next to it, which rounds to the code that
-// it rounds to itself.  By whole wavefronts.
+// it rounds to itself.  By whole wavefronts.  How many chunks that are depends on the values: 5 % of normal ones, 24 % where one column is
+// 1000 times the others, 65 % where one in every block is 100 times the others; in a captured graph 16384 x 2048 then take 62.5, 62.1 and 67.7 us,
+// 2048 x 768 6.6, 7.0 and 7.3, one row 3.1, 3.4 and 3.5.
 __device__ __forceinline__ void exact_codes(const float (&s)[8], const float* w, int c, int d, float rho, uint32_t most, float (&n)[8]) {
     double u[8], top = 0.0;
 #pragma unroll
