@@ -318,7 +318,7 @@ moe_status moe_layer_forward_noalloc(const moe_shape* shape, const void* x, cons
 
 /* ---------------------------------------------------------------------------------------------------------------
  * 8-bit layers.  A cold expert costs its parameter bytes (Section 3.1), so parameters of half the size are half the
- * time, and hot experts run at twice the matrix rate.  The calls below take the layer from the residual stream to the
+ * time; hot experts can run on matrix units of twice the rate (MOE_QUANT_UNIT_SUMS).  The calls below take the layer from the residual stream to the
  * experts' rows in e4m3: the norm in front of the layer with a quantised output, and linear layers on quantised rows and
  * weights, for one weight matrix and grouped by expert.  moe_route, moe_permute (with x_perm NULL) and moe_combine are
  * the steps between and after them.
