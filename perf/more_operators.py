@@ -147,7 +147,7 @@ def _laid_out(w):
 
     E, N, K = w.shape
     packed = torch.empty(moe.moe_quant_weight_bytes(E, N, K), dtype=torch.int8, device="cuda")
-    moe.moe_quantize_weights_i8(E, N, K, "i8", w, packed, None)
+    moe.moe_quantize_weights_int(E, N, K, "i8", w, packed, None)
     return packed
 
 
@@ -179,7 +179,7 @@ def _buffers_of_product(s, c):
     A = c["T"] * c.get("k", 1)
     s["packed"] = _laid_out(s["w"])
     s["shape"] = moe.make_quant_shape(A, c["N"], c["K"], c.get("E", 1), c.get("k", 1), c["act"], c["out"])
-    s["ws"] = torch.empty(max(256, moe.moe_i8_workspace_bytes(s["shape"])), dtype=torch.uint8, device="cuda")
+    s["ws"] = torch.empty(max(256, moe.moe_int_workspace_bytes(s["shape"])), dtype=torch.uint8, device="cuda")
 
 
 def prepare(case, seed):
@@ -258,15 +258,15 @@ def _run_own(s):
                              c["H"], s["hot"], s["ws"])
         return _route_out(s["idx"], s["weight"], s["counts"], s["offsets"], s["hot"])
     if c["op"] == "norm":
-        moe.moe_norm_quantize_i8(c["T"], c["d"], c["dtype"], s["x"], s["residual"], s["weight"], EPS, s["sum"], s["normed"], s["q"], s["scales"])
+        moe.moe_norm_quantize_int(c["T"], c["d"], c["dtype"], s["x"], s["residual"], s["weight"], EPS, s["sum"], s["normed"], s["q"], s["scales"])
         return _norm_out(s["sum"], s["normed"], s["q"][:, :c["d"]], s["scales"])
     if c["op"] == "act":
-        moe.moe_act_quantize_i8(c["T"], c["f"], c["dtype"], s["h"], c["gated"], c["act"], 0, None, None, s["q"], s["scales"])
+        moe.moe_act_quantize_int(c["T"], c["f"], c["dtype"], s["h"], c["gated"], c["act"], 0, None, None, s["q"], s["scales"])
         return {"q": s["q"][:, :c["f"]], "scales": s["scales"]}
     if c["op"] == "linear":
-        moe.moe_i8_linear(s["shape"], s["q"], s["q_scales"], s["packed"], s["w_scales"], s["bias"], s["out"], s["ws"])
+        moe.moe_int_linear(s["shape"], s["q"], s["q_scales"], s["packed"], s["w_scales"], s["bias"], s["out"], s["ws"])
         return s["out"]
-    moe.moe_i8_expert_linear(s["shape"], s["q"], s["q_scales"], s["perm"] if c["gather"] else None, s["offsets"], s["mask"], s["packed"],
+    moe.moe_int_expert_linear(s["shape"], s["q"], s["q_scales"], s["perm"] if c["gather"] else None, s["offsets"], s["mask"], s["packed"],
                              s["w_scales"], s["bias"], s["out"], s["ws"])
     return s["out"]
 
