@@ -55,12 +55,14 @@ typedef enum {
 } moe_status;
 
 typedef enum { MOE_F32 = 0, MOE_BF16 = 1,
-               MOE_E4M3 = 2     /* 8 bits (OCP e4m3: 3 bits of mantissa, largest value 448, no infinities): moe_quant_* only */
+               MOE_E4M3 = 2,    /* 8 bits (OCP e4m3: 3 bits of mantissa, largest value 448, no infinities): moe_quant_* only */
+               MOE_I8 = 3       /* signed 8-bit integers: moe_quantize_weights_int only */
 } moe_dtype;
 
 /* trailing activation of an expert's first linear layer (Section 3.4: "ReLU or GeLU") */
 typedef enum { MOE_ACT_RELU = 0, MOE_ACT_GELU = 1,
-               MOE_ACT_NONE = -1    /* moe_quant_* only */
+               MOE_ACT_SILU = 2,    /* z / (1 + exp(-z)): int8 layers only */
+               MOE_ACT_NONE = -1    /* moe_quant_* and int8 layers only */
 } moe_activation;
 
 typedef struct {
@@ -406,6 +408,105 @@ moe_status moe_quant_linear(const moe_quant_shape* shape, const void* a, const f
 moe_status moe_quant_expert_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const int32_t* perm,
                                    const int32_t* offsets, const uint8_t* mask, const void* w, const float* w_scales, const float* bias,
                                    void* out, float* out_scales, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Routing by scores.  moe_route takes softmax probabilities as they are; the two calls below are the router of layers that keep their
+ * experts balanced by a bias and their tokens within groups of experts.  They take the place of moe_route; moe_permute, the products and
+ * moe_combine follow as before.
+ */
+
+/*
+ * Router logits: logits [T, E] fp32 = x . w_gate^T + gate_bias.  x [T, d], w_gate [E, d] of the shape's dtype, gate_bias [E] fp32 or NULL;
+ * sums are fp32.  k, d_ff, renormalize and activation play no part.  T == 0 is a no-op.
+ */
+moe_status moe_gate_logits(const moe_shape* shape, const void* x, const void* w_gate, const float* gate_bias, float* logits, void* stream);
+
+typedef enum { MOE_SCORE_SOFTMAX = 0, MOE_SCORE_SIGMOID = 1 } moe_score;
+
+#define MOE_MAX_GROUPS 64
+
+typedef struct {
+    int32_t score;         /* moe_score: p = softmax over the token's logits, or sigmoid of each                */
+    int32_t groups;        /* groups of E / groups neighbouring experts (E % groups == 0), at most MOE_MAX_GROUPS   */
+    int32_t groups_kept;   /* groups that a token's experts come from; groups_kept * E / groups >= k             */
+    int32_t group_top;     /* 1 or 2: a group's value is the sum of that many largest choices (2 <= E / groups)    */
+    float scale;           /* finite; multiplies the weights                                                 */
+} moe_routing;
+
+/*
+ * Routing from logits [T, E] of logits_dtype (MOE_F32 or MOE_BF16).  choice_bias [E] fp32 or NULL: added to the scores for the choice alone.
+ *   c[t, e] = p[t, e] + choice_bias[e];  without a bias experts are ordered by their logits, which is the order of p without its rounding;
+ *   group value: the largest c of the group, or the sum of the two largest (without a bias: of p); the groups_kept groups of the largest
+ *                values, equal ones ordered by lowest index;
+ *   topk_idx [T, k]: the experts of the k largest c in the kept groups, descending, equal ones ordered by lowest index;
+ *   topk_w  [T, k]: p of these (shape->renormalize: divided by their sum; zero where that is zero), times scale;
+ *   counts [E], offsets [E + 1], H, hot_mask: as moe_route.
+ * Scores are compared in 64 bits, so that the choice is the formulas', however close two of them are.
+ * A logit of -infinity marks an expert that is not there: it is chosen after all others (so only where fewer than k are left, lowest index
+ * first, with weight zero), and so is one whose c is NaN.  The weights of a token with a NaN among its logits (softmax: or +infinity) are NaN.
+ * T, E, k and renormalize of `shape` enter, dtype and widths need only be valid.  ws: at least moe_workspace_bytes(shape).
+ */
+moe_status moe_route_logits(const moe_shape* shape, const moe_routing* routing, int32_t logits_dtype, const void* logits,
+                            const float* choice_bias, int32_t* topk_idx, float* topk_w, int32_t* counts, int32_t* offsets, int32_t H,
+                            uint8_t* hot_mask, void* ws, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * int8 layers: rows and weights as 8-bit integers, with one fp32 scale per row (token) and per output channel.  Half the bytes of bf16
+ * weights, as the e4m3 layers above; sums are exact, so that results do not depend on how a product is cut.
+ *
+ * int8 rows [R, C]: codes -127 ... 127 in rows of moe_quant_pitch(C) bytes (the codes past C are zero) and scales [R]; value (r, c) is
+ * code(r, c) * scale(r).  As these calls write them, a row of values v has scale = max(max |v| / 127, 2^-126) and code = the whole number next
+ * to v / (max |v| / 127), ties to even, of v and the quotient as real numbers: where fp32 leaves a doubt, 64 bits decide.  A row that holds a
+ * NaN, an infinity or a value beyond fp32's range has a NaN for its scale and codes of zero, so that products with it are NaN.
+ * int8 weights of E matrices [N, K]: scales [E, N], and the codes in the products' layout, made once by moe_quantize_weights_int; their size is
+ * moe_quant_weight_bytes.  The products take any codes (-128 too) and any scales whose products sa * sw stay within fp32.
+ * Codes and packed weights are 16-byte aligned, other pointers to the size of their elements.
+ */
+#define MOE_INT_MAX_K 131071
+
+/*
+ * One-time weight preparation.  src [E, N, K], row-major, of type src_dtype:
+ *   MOE_F32, MOE_BF16: quantised; scales [E, N] = max(max |w| / 127, 2^-126) over each row, code = w / scale, rounded to fp32 and from there to
+ *   the nearest whole number; a row that holds a NaN or an infinity has a NaN for its scale and codes of zero.
+ *   MOE_I8: a checkpoint's own codes, laid out as they are; their scales are the caller's and `scales` is not used (NULL).
+ * dst: moe_quant_weight_bytes(E, N, K) bytes, laid out as moe_quantize_weights does.  src and dst must not overlap.
+ * 1 <= E <= 1024, 1 <= N <= 2^24, 1 <= K <= MOE_INT_MAX_K.
+ */
+moe_status moe_quantize_weights_int(int32_t E, int32_t N, int32_t K, int32_t src_dtype, const void* src, void* dst, float* scales, void* stream);
+
+/* moe_norm_quantize with int8 rows: q, q_scales [rows].  Everything else as there, but for rows whose squares' sum fp32 does not hold: theirs is
+ * a sum in 64 bits. */
+moe_status moe_norm_quantize_int(int32_t rows, int32_t d, int32_t dtype, const void* x, const void* residual, const float* weight, float eps,
+                                 void* sum_out, void* norm_out, void* q, float* q_scales, void* stream);
+
+/*
+ * What lies between a layer's two products: the activation, and its values as int8 rows (a row's scale is that of all its values, which no
+ * product's own units see).
+ *   gated == 0: h [rows, f] of dtype MOE_F32 or MOE_BF16, v = act(h);   gated == 1: h [rows, 2 f], v = act(h[:, :f]) * h[:, f:].
+ *   activation: moe_activation, MOE_ACT_NONE among them.  q, q_scales: v as int8 rows [rows, f].
+ *   offsets NULL: all rows (E and mask play no part).  offsets [E + 1] (device): rows that belong to no expert, or with mask [E] != NULL to one
+ *   with mask[e] == 0, are neither read nor written.
+ * rows >= 0 (0: a no-op), 1 <= f <= 2^24.  h and q must not overlap.
+ */
+moe_status moe_act_quantize_int(int32_t rows, int32_t f, int32_t dtype, const void* h, int32_t gated, int32_t activation, int32_t E,
+                                const int32_t* offsets, const uint8_t* mask, void* q, float* q_scales, void* stream);
+
+/* Bytes of workspace of the two calls below (0 on a shape that they refuse; rows == 0, a no-op, is none). */
+size_t moe_int_workspace_bytes(const moe_quant_shape* shape);
+
+/*
+ * out[r, n] = act( sa[r] * sw[n] * sum_c a[r, c] * w[n, c] + bias[n] )
+ * a, sa: int8 rows [rows, K]; w, sw: packed weights and their scales (E = 1); bias [N] fp32 or NULL; out [rows, N] of shape->out_dtype, MOE_F32 or
+ * MOE_BF16.  The sum is exact, what follows fp32, rounded once to out_dtype.  K <= MOE_INT_MAX_K.  ws: at least moe_int_workspace_bytes,
+ * 256-byte aligned.  Outputs overlap nothing.
+ */
+moe_status moe_int_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const void* w, const float* w_scales,
+                          const float* bias, void* out, void* ws, size_t ws_bytes, void* stream);
+
+/* The same for E weight matrices and rows grouped by expert: perm, offsets and mask as moe_quant_expert_linear takes them. */
+moe_status moe_int_expert_linear(const moe_quant_shape* shape, const void* a, const float* a_scales, const int32_t* perm,
+                                 const int32_t* offsets, const uint8_t* mask, const void* w, const float* w_scales, const float* bias,
+                                 void* out, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

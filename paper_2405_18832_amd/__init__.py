@@ -17,11 +17,13 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("MOE_FFN_LIB") or os.path.join(_PKG, "libmoe_ffn_gfx950.so")
 
 MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP = range(5)
-MOE_F32, MOE_BF16, MOE_E4M3 = 0, 1, 2
-MOE_ACT_NONE, MOE_ACT_RELU, MOE_ACT_GELU = -1, 0, 1
+MOE_F32, MOE_BF16, MOE_E4M3, MOE_I8 = 0, 1, 2, 3
+MOE_ACT_NONE, MOE_ACT_RELU, MOE_ACT_GELU, MOE_ACT_SILU = -1, 0, 1, 2
+MOE_SCORE_SOFTMAX, MOE_SCORE_SIGMOID = 0, 1
 MOE_QUANT_BLOCK = 128
 MOE_QUANT_UNIT_SUMS = 0x100
-MOE_MAX_K, MOE_MAX_E = 8, 1024
+MOE_MAX_K, MOE_MAX_E, MOE_MAX_GROUPS = 8, 1024, 64
+MOE_INT_MAX_K = 131071
 
 EXPORTS = ["moe_init", "moe_noalloc_max_workspace", "moe_layer_forward_noalloc",
            "moe_status_string", "moe_workspace_bytes", "moe_packed_weight_bytes", "moe_pack_weights",
@@ -30,7 +32,9 @@ EXPORTS = ["moe_init", "moe_noalloc_max_workspace", "moe_layer_forward_noalloc",
            "moe_route", "moe_select_hot", "moe_permute", "moe_expert_ffn", "moe_expert_ffn_biased", "moe_combine",
            "moe_layer_forward", "moe_layer_forward_biased",
            "moe_quant_pitch", "moe_quant_weight_bytes", "moe_quantize_weights", "moe_norm_quantize", "moe_quant_workspace_bytes",
-           "moe_quant_linear", "moe_quant_expert_linear"]
+           "moe_quant_linear", "moe_quant_expert_linear",
+           "moe_gate_logits", "moe_route_logits", "moe_quantize_weights_int", "moe_norm_quantize_int", "moe_act_quantize_int",
+           "moe_int_workspace_bytes", "moe_int_linear", "moe_int_expert_linear"]
 
 
 class MoEError(RuntimeError):
@@ -46,6 +50,10 @@ class moe_shape(ctypes.Structure):
 
 class moe_quant_shape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("rows", "N", "K", "E", "k", "activation", "out_dtype")]
+
+
+class moe_routing(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("score", "groups", "groups_kept", "group_top")] + [("scale", ctypes.c_float)]
 
 
 _lib = None
@@ -125,6 +133,22 @@ def load() -> ctypes.CDLL:
     lib.moe_quant_linear.restype = ctypes.c_int
     lib.moe_quant_expert_linear.argtypes = [qp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.moe_quant_expert_linear.restype = ctypes.c_int
+    lib.moe_gate_logits.argtypes = [sp, vp, vp, vp, vp, vp]
+    lib.moe_gate_logits.restype = ctypes.c_int
+    lib.moe_route_logits.argtypes = [sp, ctypes.POINTER(moe_routing), i32, vp, vp, vp, vp, vp, vp, i32, vp, vp, sz, vp]
+    lib.moe_route_logits.restype = ctypes.c_int
+    lib.moe_quantize_weights_int.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp]
+    lib.moe_quantize_weights_int.restype = ctypes.c_int
+    lib.moe_norm_quantize_int.argtypes = [i32, i32, i32, vp, vp, vp, ctypes.c_float, vp, vp, vp, vp, vp]
+    lib.moe_norm_quantize_int.restype = ctypes.c_int
+    lib.moe_act_quantize_int.argtypes = [i32, i32, i32, vp, i32, i32, i32, vp, vp, vp, vp, vp]
+    lib.moe_act_quantize_int.restype = ctypes.c_int
+    lib.moe_int_workspace_bytes.argtypes = [qp]
+    lib.moe_int_workspace_bytes.restype = sz
+    lib.moe_int_linear.argtypes = [qp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_int_linear.restype = ctypes.c_int
+    lib.moe_int_expert_linear.argtypes = [qp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.moe_int_expert_linear.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -140,8 +164,9 @@ def make_shape(T, d_model, d_ff, E, k, dtype, renormalize, activation=0) -> moe_
                      int(bool(renormalize)), int(activation))
 
 
-_DTYPE_NAMES = {"f32": MOE_F32, "bf16": MOE_BF16, "e4m3": MOE_E4M3}
-_ACT_NAMES = {"none": MOE_ACT_NONE, "relu": MOE_ACT_RELU, "gelu": MOE_ACT_GELU}
+_DTYPE_NAMES = {"f32": MOE_F32, "bf16": MOE_BF16, "e4m3": MOE_E4M3, "i8": MOE_I8}
+_ACT_NAMES = {"none": MOE_ACT_NONE, "relu": MOE_ACT_RELU, "gelu": MOE_ACT_GELU, "silu": MOE_ACT_SILU}
+_SCORE_NAMES = {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}
 
 
 def make_quant_shape(rows, N, K, E=1, k=1, activation="none", out_dtype="bf16", sums="f32") -> moe_quant_shape:
@@ -149,6 +174,11 @@ def make_quant_shape(rows, N, K, E=1, k=1, activation="none", out_dtype="bf16", 
     the matrix units for 8-bit operands (MOE_QUANT_UNIT_SUMS: faster for many rows, less exact; bf16 and e4m3 outputs)."""
     out = int(_DTYPE_NAMES.get(out_dtype, out_dtype)) | {"f32": 0, "units": MOE_QUANT_UNIT_SUMS}[sums]
     return moe_quant_shape(int(rows), int(N), int(K), int(E), int(k), int(_ACT_NAMES.get(activation, activation)), out)
+
+
+def make_routing(score="softmax", groups=1, groups_kept=1, group_top=1, scale=1.0) -> moe_routing:
+    """`score`: "softmax" | "sigmoid" (or the C value)."""
+    return moe_routing(int(_SCORE_NAMES.get(score, score)), int(groups), int(groups_kept), int(group_top), float(scale))
 
 
 def _ptr(t) -> Optional[int]:
@@ -356,3 +386,45 @@ def moe_quant_expert_linear(shape, a, a_scales, perm, offsets, mask, w, w_scales
     _check(load().moe_quant_expert_linear(ctypes.byref(shape), _ptr(a), _ptr(a_scales), _ptr(perm), _ptr(offsets), _ptr(mask),
                                           _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(out), _ptr(out_scales), _ptr(ws), _nbytes(ws),
                                           _stream(stream)), "moe_quant_expert_linear")
+
+
+# ---- routing by scores, int8 layers ---------------------------------------------------------------------------------
+# int8 rows and packed weights are one-byte tensors (torch.int8 or torch.uint8).
+def moe_gate_logits(shape, x, w_gate, gate_bias, logits, stream=None) -> None:
+    _check(load().moe_gate_logits(ctypes.byref(shape), _ptr(x), _ptr(w_gate), _ptr(gate_bias), _ptr(logits), _stream(stream)), "moe_gate_logits")
+
+
+def moe_route_logits(shape, routing, logits_dtype, logits, choice_bias, topk_idx, topk_w, counts, offsets, H, hot_mask, ws, stream=None) -> None:
+    _check(load().moe_route_logits(ctypes.byref(shape), ctypes.byref(routing), int(_DTYPE_NAMES.get(logits_dtype, logits_dtype)), _ptr(logits),
+                                   _ptr(choice_bias), _ptr(topk_idx), _ptr(topk_w), _ptr(counts), _ptr(offsets), int(H), _ptr(hot_mask), _ptr(ws),
+                                   _nbytes(ws), _stream(stream)), "moe_route_logits")
+
+
+def moe_quantize_weights_int(E, N, K, src_dtype, src, dst, scales, stream=None) -> None:
+    _check(load().moe_quantize_weights_int(int(E), int(N), int(K), int(_DTYPE_NAMES.get(src_dtype, src_dtype)), _ptr(src), _ptr(dst), _ptr(scales),
+                                           _stream(stream)), "moe_quantize_weights_int")
+
+
+def moe_norm_quantize_int(rows, d, dtype, x, residual, weight, eps, sum_out, norm_out, q, q_scales, stream=None) -> None:
+    _check(load().moe_norm_quantize_int(int(rows), int(d), int(_DTYPE_NAMES.get(dtype, dtype)), _ptr(x), _ptr(residual), _ptr(weight), float(eps),
+                                        _ptr(sum_out), _ptr(norm_out), _ptr(q), _ptr(q_scales), _stream(stream)), "moe_norm_quantize_int")
+
+
+def moe_act_quantize_int(rows, f, dtype, h, gated, activation, E, offsets, mask, q, q_scales, stream=None) -> None:
+    _check(load().moe_act_quantize_int(int(rows), int(f), int(_DTYPE_NAMES.get(dtype, dtype)), _ptr(h), int(gated),
+                                       int(_ACT_NAMES.get(activation, activation)), int(E), _ptr(offsets), _ptr(mask), _ptr(q), _ptr(q_scales),
+                                       _stream(stream)), "moe_act_quantize_int")
+
+
+def moe_int_workspace_bytes(shape: moe_quant_shape) -> int:
+    return int(load().moe_int_workspace_bytes(ctypes.byref(shape)))
+
+
+def moe_int_linear(shape, a, a_scales, w, w_scales, bias, out, ws, stream=None) -> None:
+    _check(load().moe_int_linear(ctypes.byref(shape), _ptr(a), _ptr(a_scales), _ptr(w), _ptr(w_scales), _ptr(bias), _ptr(out), _ptr(ws), _nbytes(ws),
+                                 _stream(stream)), "moe_int_linear")
+
+
+def moe_int_expert_linear(shape, a, a_scales, perm, offsets, mask, w, w_scales, bias, out, ws, stream=None) -> None:
+    _check(load().moe_int_expert_linear(ctypes.byref(shape), _ptr(a), _ptr(a_scales), _ptr(perm), _ptr(offsets), _ptr(mask), _ptr(w), _ptr(w_scales),
+                                        _ptr(bias), _ptr(out), _ptr(ws), _nbytes(ws), _stream(stream)), "moe_int_expert_linear")

@@ -51,6 +51,8 @@ template <typename T> inline T* at(void* ws, size_t off) {
 
 namespace moe {
 
+moe_status layer_shape_status(const moe_shape* s) { return check_shape(s); }
+
 int current_device_index() {
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxDevices) return 0;
@@ -70,6 +72,8 @@ hipError_t ensure_ready() {
     if ((e = configure_f32_kernels()) != hipSuccess) return e;
     if ((e = configure_route_kernels(dev)) != hipSuccess) return e;
     if ((e = configure_quant_kernels()) != hipSuccess) return e;
+    if ((e = configure_int_kernels()) != hipSuccess) return e;
+    if ((e = configure_score_kernels()) != hipSuccess) return e;
     // this device's copy of the scratch array (each GPU has its own, at its own address)
     void* p = nullptr;
     if ((e = hipGetSymbolAddress(&p, HIP_SYMBOL(scratch))) != hipSuccess) return e;

@@ -491,11 +491,14 @@ int device_cu_count();
 constexpr int kMaxDevices = 64;
 constexpr size_t kLdsPerCu = 160 * 1024;
 hipError_t ensure_ready();                       // api.hip
+moe_status layer_shape_status(const moe_shape* s);      // api.hip: whether the layer's calls take this shape
 int current_device_index();                      // api.hip: hipGetDevice clamped to [0, kMaxDevices)
 hipError_t configure_ffn_kernels(int dev);       // ffn.hip
 hipError_t configure_tile_kernels(int dev);      // ffn_tile.hip
 hipError_t configure_f32_kernels();              // ffn_f32.hip
 hipError_t configure_route_kernels(int dev);     // route.hip
 hipError_t configure_quant_kernels();            // quant_linear.hip
+hipError_t configure_int_kernels();              // int_linear.hip
+hipError_t configure_score_kernels();            // score_route.hip
 
 }  // namespace moe
