@@ -47,6 +47,7 @@ hipError_t launch_int_product(const QuantArgs& a, void* ws, hipStream_t stream);
 hipError_t launch_gate_logits(const moe_shape& s, const void* x, const void* w_gate, const float* bias, float* logits, hipStream_t stream);
 struct ScoreArgs {
     const void* logits;
+    bool bf16;                          // logits' type: bf16, else fp32
     const float* balance;
     int32_t* idx;
     float* weight;
@@ -58,6 +59,6 @@ struct ScoreArgs {
     int groups, kept, top;
     float scale;
 };
-hipError_t launch_route_logits(const ScoreArgs& a, int logits_dtype, hipStream_t stream);
+hipError_t launch_route_logits(const ScoreArgs& a, hipStream_t stream);
 
 }  // namespace moe

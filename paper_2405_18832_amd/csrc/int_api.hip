@@ -101,11 +101,11 @@ moe_status moe_route_logits(const moe_shape* shape, const moe_routing* routing, 
         return MOE_ERR_INVALID_ARG;
     if (ws == nullptr || !aligned(ws, 256) || ws_bytes < ws_layout(*shape).total) return MOE_ERR_WORKSPACE;
     if (ensure_ready() != hipSuccess) return MOE_ERR_HIP;
-    const ScoreArgs args{logits, choice_bias, topk_idx, topk_w, counts, offsets, hot_mask,
+    const ScoreArgs args{logits, logits_dtype == MOE_BF16, choice_bias, topk_idx, topk_w, counts, offsets, hot_mask,
                          reinterpret_cast<int32_t*>(static_cast<char*>(ws) + ws_layout(*shape).hist),
                          shape->T, shape->E, shape->k, H, routing->score == MOE_SCORE_SIGMOID, shape->renormalize != 0,
                          routing->groups, routing->groups_kept, routing->group_top, routing->scale};
-    return from_hip(launch_route_logits(args, logits_dtype, static_cast<hipStream_t>(stream)));
+    return from_hip(launch_route_logits(args, static_cast<hipStream_t>(stream)));
 }
 
 moe_status moe_quantize_weights_int(int32_t E, int32_t N, int32_t K, int32_t src_dtype, const void* src, void* dst, float* scales, void* stream) {
