@@ -21,14 +21,24 @@ __device__ __forceinline__ i32x4 multiply(const i32x8& w, const i32x8& x, i32x4 
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_shufflevector(w, w, 4, 5, 6, 7), __builtin_shufflevector(x, x, 4, 5, 6, 7), sum, 0, 0, 0);
 }
 
+// SMOOTH: GeLU or SiLU, else none or ReLU, the kernels' variants (every one in each of a kernel's many epilogues is more code than its cache holds).
+bool is_smooth(int act) { return act == MOE_ACT_GELU || act == MOE_ACT_SILU; }
+template <bool SMOOTH>
 __device__ __forceinline__ float int_activate(float v, int act) {
-    if (act == MOE_ACT_RELU) return v < 0.f ? 0.f : v;      // NaN stays
-    if (act == MOE_ACT_GELU) return gelu_exp(v);
-    if (act == MOE_ACT_SILU) return silu(v);
+    if constexpr (SMOOTH) return act == MOE_ACT_GELU ? gelu_exp(v) : silu(v);
+    const float least = act == MOE_ACT_RELU ? 0.f : -__builtin_huge_valf();
+    return v < least ? least : v;                           // NaN stays
+}
+// A lane's sums of a fragment of 16 columns x 16 rows as values: sx of its row, sw and bias of its four columns.
+template <bool SMOOTH>
+__device__ __forceinline__ f32x4 finish_fragment(int act, float sx, const f32x4& w, const f32x4& b, const i32x4& sums) {
+    f32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = int_activate<SMOOTH>(fmaf(static_cast<float>(sums[i]), sx * w[i], b[i]), act);
     return v;
 }
-// A lane's sums of NF fragments of columns x TF of rows as values: sx of its rows, sw and bias of its columns (four of each fragment), in LDS.
-template <int NF, int TF>
+// The same for NF fragments of columns x TF of rows; sw and bias (or NULL): the lane's columns' in LDS.
+template <bool SMOOTH, int NF, int TF>
 __device__ __forceinline__ void finish(int act, const float (&sx)[TF], const unsigned char* sw, const unsigned char* bias, const i32x4 (&sums)[NF][TF],
                                        f32x4 (&v)[NF][TF]) {
 #pragma unroll
@@ -37,19 +47,11 @@ __device__ __forceinline__ void finish(int act, const float (&sx)[TF], const uns
         f32x4 b = {0.f, 0.f, 0.f, 0.f};
         if (bias != nullptr) b = *reinterpret_cast<const f32x4*>(bias + nf * 64);
 #pragma unroll
-        for (int tf = 0; tf < TF; ++tf)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[nf][tf][i] = fmaf(static_cast<float>(sums[nf][tf][i]), sx[tf] * w[i], b[i]);
-    }
-    if (act == MOE_ACT_NONE) return;
-#pragma unroll
-    for (int nf = 0; nf < NF; ++nf)
-#pragma unroll
         for (int tf = 0; tf < TF; ++tf) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[nf][tf][i] = int_activate(v[nf][tf][i], act);
+            v[nf][tf] = finish_fragment<SMOOTH>(act, sx[tf], w, b, sums[nf][tf]);
             if (NF * TF > 4) __builtin_amdgcn_sched_barrier(0);        // many values at once would need registers that there are not
         }
+    }
 }
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
@@ -70,7 +72,7 @@ struct Streams {
 // OUT = kOutParts: the contraction is cut into `split` parts, whose sums go to a.out as [split][rows][pitch of N] int32.
 constexpr int kOutParts = 3;
 
-template <int OUT, int NF>
+template <int OUT, int NF, bool SMOOTH>
 __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t* list, int tiles, int parts_wanted, int b, unsigned char* smem) {
     using S = Streams<NF>;
     constexpr int kStages = S::kStages, kStage = S::kStage;
@@ -236,7 +238,7 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
 #pragma unroll
                 for (int tf = 0; tf < TF; ++tf) sx[tf] = *reinterpret_cast<const float*>(of + (tf * 16 + r) * 4);
                 f32x4 v[NF][TF];
-                finish(a.act, sx, of + S::kSw + at_columns, a.bias != nullptr ? of + S::kBias + at_columns : nullptr, acc, v);
+                finish<SMOOTH>(a.act, sx, of + S::kSw + at_columns, a.bias != nullptr ? of + S::kBias + at_columns : nullptr, acc, v);
                 store_values<OUT, 16>(a, n0, cur.row0, cur.rows, v);
                 unit = unit == S::kPlaces - 1 ? 0 : unit + 1;
             }
@@ -255,16 +257,16 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
 constexpr int kListAt = Streams<1>::kList > Streams<2>::kList ? Streams<1>::kList : Streams<2>::kList;      // behind both rings
 constexpr int kStreamLds = kListAt + MOE_MAX_E * 2 + kStreamWaves * 4;
 
-template <int OUT>
+template <int OUT, bool SMOOTH>
 __global__ __launch_bounds__(kStreamWaves * 64) void int_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + kListAt);
     const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
-    stream_units<OUT, 1>(a, list, tiles, parts_wanted, blockIdx.x, smem);
+    stream_units<OUT, 1, SMOOTH>(a, list, tiles, parts_wanted, blockIdx.x, smem);
 }
 
 // Adds up the parts of a split contraction and finishes the rows.  A block of threads per row and 1024 columns, four per thread.
-template <int OUT>
+template <int OUT, bool SMOOTH>
 __global__ __launch_bounds__(256) void int_join_kernel(const QuantArgs a, const int32_t* __restrict__ parts, int split) {
     const int row = blockIdx.x, n0 = (blockIdx.y * 256 + threadIdx.x) * 4;
     const size_t pitch = quant_pitch(a.N);
@@ -287,7 +289,7 @@ __global__ __launch_bounds__(256) void int_join_kernel(const QuantArgs a, const 
     for (int i = 0; i < 4; ++i)
         if (n0 + i < a.N) {
             const size_t of = static_cast<size_t>(e) * a.N + n0 + i, at = static_cast<size_t>(row) * a.N + n0 + i;
-            const float v = int_activate(fmaf(static_cast<float>(sum[i]), sx * a.w_scales[of], a.bias != nullptr ? a.bias[of] : 0.f), a.act);
+            const float v = int_activate<SMOOTH>(fmaf(static_cast<float>(sum[i]), sx * a.w_scales[of], a.bias != nullptr ? a.bias[of] : 0.f), a.act);
             if constexpr (OUT == kOutF32) static_cast<float*>(a.out)[at] = v;
             else static_cast<uint16_t*>(a.out)[at] = f32_to_bf16(v);
         }
@@ -298,7 +300,7 @@ __global__ __launch_bounds__(256) void int_join_kernel(const QuantArgs a, const 
 // LDS stages that runs on across units.  Everything goes from memory to LDS directly, 16 bytes per lane; a stage holds
 //   rows     [64 RMAX][128 bytes]
 //   weights  8 fragments of 2 KiB as they are packed, 16 rows each
-// and a unit's scales and biases go before its first stage to a place of their own, one more than there are stages, for units of one step.
+// and a unit's scales and biases go before its first stage to a place of their own, one more than there are stages.
 // Wavefront (wm, wn) of the 4 x 2 multiplies row fragments wm, wm + 4, ... (R of them) and the columns 64 wn ... 64 wn + 63.
 constexpr int kTileWaves = 8;
 template <int RMAX>
@@ -312,7 +314,8 @@ struct Tiles {
     static_assert(kLdsBytes <= 160 * 1024, "fits a CU");
 };
 
-template <int OUT, int RMAX>
+// PASS: the output passes by the caches.
+template <int OUT, int RMAX, bool SMOOTH, bool PASS>
 __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, unsigned char* smem) {
     using T = Tiles<RMAX>;
     constexpr int kStages = T::kStages, kStageW = T::kStageW, kStage = T::kStage, tile_rows = T::kRows;
@@ -390,104 +393,295 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
     Unit ahead = unit_at(u_in);
     point_at(ahead);
     int kb_in = 0, slot_in = 0;
-    bool copying = true;
-    auto copy_next = [&]() __attribute__((always_inline)) {
+    // The ring runs on across units: the next unit's first stages go out during the last steps of this one.  Behind the last unit the
+    // last stage is copied again, which keeps up the count that the waits go by.
+    auto copy_piece = [&](int n) __attribute__((always_inline)) {
         const int at = slot_in * kStage;
-#pragma unroll
-        for (int i = 0; i < RMAX; ++i) {
-            if constexpr (OFFSETS) copy16_to_lds(rows_base, row_offset[i], to_rows + at + i * 8192);
-            else copy16_to_lds(row_from[i], to_rows + at + i * 8192);
+        if (n < RMAX) {
+            if constexpr (OFFSETS) copy16_to_lds(rows_base, row_offset[n < RMAX ? n : 0], to_rows + at + n * 8192);
+            else copy16_to_lds(row_from[n < RMAX ? n : 0], to_rows + at + n * 8192);
+        } else if (n < RMAX + 2) {
+            copy16_to_lds(weights_base + (n - RMAX) * 1024, lane16, to_weights + at + (n - RMAX) * 1024);
         }
-        copy16_to_lds(weights_base, lane16, to_weights + at);
-        copy16_to_lds(weights_base + 1024, lane16, to_weights + at + 1024);
+    };
+    uint32_t stage_step = 1;               // 0 behind the last unit
+    auto next_stage = [&]() __attribute__((always_inline)) {
         slot_in = slot_in == kStages - 1 ? 0 : slot_in + 1;
-        if (copying) {                     // behind the last unit its last stage is copied again, which keeps up the count that the waits go by
-            if (++kb_in == KB) {
-                kb_in = 0;
-                if (u_in + static_cast<int>(gridDim.x) < units) {
-                    u_in += gridDim.x;
-                    ahead = unit_at(u_in);
-                    point_at(ahead);
-                } else {
-                    copying = false;
-                }
-            } else {
-                weights_base += kFragBytes;
-                if constexpr (OFFSETS) {
-                    rows_base += kQuantBlock;
-                } else {
+        weights_base += stage_step * kFragBytes;
+        if constexpr (OFFSETS) {
+            rows_base += stage_step * kQuantBlock;
+        } else {
 #pragma unroll
-                    for (int i = 0; i < RMAX; ++i) row_from[i] += kQuantBlock;
-                }
+            for (int i = 0; i < RMAX; ++i) row_from[i] += stage_step * kQuantBlock;
+        }
+    };
+    // when all of a unit's stages have been sent for (kb_in == KB)
+    auto next_unit = [&]() __attribute__((always_inline)) {
+        kb_in = 0;
+        if (u_in + static_cast<int>(gridDim.x) < units) {
+            u_in += gridDim.x;
+            ahead = unit_at(u_in);
+            point_at(ahead);
+        } else if (stage_step != 0) {      // back to the last stage, which is copied from now on
+            weights_base -= kFragBytes;
+            if constexpr (OFFSETS) {
+                rows_base -= kQuantBlock;
+            } else {
+#pragma unroll
+                for (int i = 0; i < RMAX; ++i) row_from[i] -= kQuantBlock;
             }
+            stage_step = 0;
         }
     };
     Unit cur = ahead;
 #pragma unroll 1
-    for (int i = 0; i < kStages - 1; ++i) copy_next();
+    for (int i = 0; i < kStages; ++i) {
+        if (kb_in == KB) next_unit();
+#pragma unroll
+        for (int n = 0; n < T::kCopies; ++n) copy_piece(n);
+        next_stage();
+        ++kb_in;
+    }
+    copies_landed<(kStages - 1) * T::kCopies>();
 
     int slot = 0, unit = 0;
+    uint32_t landed = 0;                    // steps from here on whose next stage is known to have landed
+    // The sums of a unit of all row fragments are finished and stored during the next one's steps, a row fragment at a time (so that no two units' results
+    // go to memory at once and the matrix units need not wait for the vector unit), where that has all fragments too and enough steps.
+    constexpr int kSpread = 2;              // steps per row fragment
+    i32x4 old[4][RMAX];
+    Unit done{0, 0, 0, 0};
+    int done_place = 0;                     // of its scales
+    bool left = false;                      // whether it is still to be finished
+    auto columns_of = [&](int place) { return smem + T::kUnits + place * T::kUnit + T::kSw + (wn * 64 + ((here(threadIdx.x) & 63) >> 4) * 4) * 4; };
+    auto row_scale = [&](int place, int i) {
+        return *reinterpret_cast<const float*>(smem + T::kUnits + place * T::kUnit + (wm * 16 + i * 64 + (here(threadIdx.x) & 15)) * 4);
+    };
+    auto store_fragments = [&](const Unit& w, int i, const f32x4 (&v)[4][1]) __attribute__((always_inline)) {
+        store_values<OUT, 64>(a, w.group * kQuantBlock + wn * 64, w.row0 + wm * 16 + i * 64, w.rows - wm * 16 - i * 64, v);
+    };
+    // Whether every store of this wavefront's part of a unit is to 16 bytes that exist, so that it takes kStores of them for a row fragment: the steps count
+    // on that number.
+    constexpr int kStores = OUT == kOutF32 ? 4 : 2;
+    auto all_exist = [&](const Unit& w) {
+        return a.N % (OUT == kOutF32 ? 4 : 8) == 0 && reinterpret_cast<uintptr_t>(a.out) % 16 == 0 && w.group * kQuantBlock + wn * 64 + 64 <= a.N &&
+               w.rows >= wm * 16 + (RMAX - 1) * 64 + 16;
+    };
+    auto store_all = [&](const Unit& w, int i, const f32x4 (&v)[4][1]) __attribute__((always_inline)) {
+        const int lane = here(threadIdx.x) & 63, g = lane >> 4;
+        const size_t at = static_cast<size_t>(w.row0 + wm * 16 + i * 64 + (lane & 15)) * a.N + w.group * kQuantBlock + wn * 64;
+        if constexpr (OUT == kOutF32) {
+#pragma unroll
+            for (int nf = 0; nf < 4; ++nf) {
+                f32x4* out = reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at + nf * 16 + g * 4);
+                if constexpr (PASS) __builtin_nontemporal_store(v[nf][0], out);
+                else *out = v[nf][0];
+            }
+        } else {
+            uint32_t lo[4], hi[4];
+#pragma unroll
+            for (int nf = 0; nf < 4; ++nf) {
+                lo[nf] = pack_bf16x2(v[nf][0][0], v[nf][0][1]);
+                hi[nf] = pack_bf16x2(v[nf][0][2], v[nf][0][3]);
+            }
+#pragma unroll
+            for (int t = 0; t < 4; t += 2) {
+                gather_pair(lo[t], lo[t + 1]);
+                gather_pair(hi[t], hi[t + 1]);
+            }
+            i32x4* out = reinterpret_cast<i32x4*>(static_cast<uint16_t*>(a.out) + at + g * 8);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const i32x4 piece = {static_cast<int>(lo[2 * t]), static_cast<int>(hi[2 * t]), static_cast<int>(lo[2 * t + 1]), static_cast<int>(hi[2 * t + 1])};
+                if constexpr (PASS) __builtin_nontemporal_store(piece, out + 4 * t);
+                else out[4 * t] = piece;
+            }
+        }
+    };
+    auto finish_now = [&](const Unit& w, int place, const auto& sums, auto fragments) __attribute__((always_inline)) {
+        // The stores are counted behind the copies in flight, which have landed when they go out; so the next unit's first steps need not wait
+        // for stores.
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        landed = kStages - 1;
+        const unsigned char* sw = columns_of(place);
+#pragma unroll
+        for (int i = 0; i < decltype(fragments)::value; ++i) {
+            const float sx = row_scale(place, i);
+            f32x4 v[4][1];
+#pragma unroll
+            for (int nf = 0; nf < 4; ++nf) {
+                f32x4 b = {0.f, 0.f, 0.f, 0.f};
+                if (a.bias != nullptr) b = *reinterpret_cast<const f32x4*>(sw + T::kBias - T::kSw + nf * 64);
+                v[nf][0] = finish_fragment<SMOOTH>(a.act, sx, *reinterpret_cast<const f32x4*>(sw + nf * 64), b, sums[nf][i]);
+                __builtin_amdgcn_sched_barrier(0);         // many values at once would need registers that there are not
+            }
+            store_fragments(w, i, v);
+        }
+    };
     auto run_unit = [&](auto fragments) __attribute__((always_inline)) {
         constexpr int R = decltype(fragments)::value;
         const int tid = here(threadIdx.x);
         const int at_x = row_operand(tid, wm * 16), x_other = row_operand_other(at_x), at_w = kStageW + wn * 4 * kFragBytes;
+        auto row_codes = [&](const unsigned char* st, int i) { return read_codes(st + at_x + i * 64 * kQuantBlock, x_other); };
+        auto weight_codes = [&](const unsigned char* st, int nf) { return read_codes(st + at_w + lane16 + nf * kFragBytes, 1024); };
         i32x4 acc[4][R];
 #pragma unroll
         for (int nf = 0; nf < 4; ++nf)
 #pragma unroll
             for (int i = 0; i < R; ++i) acc[nf][i] = i32x4{0, 0, 0, 0};
-#pragma unroll 1
-        for (int kb = 0; kb < KB; ++kb) {
-            copies_landed<(kStages - 2) * T::kCopies>();
-            const unsigned char* st = smem + slot * kStage;
-            i32x8 w[4], x[R];
+        // A step is 4 R pairs of matrix instructions: the first two weight fragments x every row fragment, then the other two.  Operands are
+        // read from the next stage into the registers of those that were used last, at least 2 R + 1 pairs (2 of one row fragment) before
+        // their use; a stage's slot is free again in the middle of its own step.  The order is held by the scheduling barriers.
+        i32x8 w[4], x[R];
+        const unsigned char* st0 = smem + slot * kStage;
 #pragma unroll
-            for (int nf = 0; nf < 4; ++nf) w[nf] = read_codes(st + at_w + lane16 + nf * kFragBytes, 1024);
+        for (int nf = 0; nf < 4; ++nf) w[nf] = weight_codes(st0, nf);
 #pragma unroll
-            for (int i = 0; i < R; ++i) x[i] = read_codes(st + at_x + i * 64 * kQuantBlock, x_other);
-            copy_next();
-#pragma unroll
-            for (int i = 0; i < R; ++i)
-#pragma unroll
-                for (int nf = 0; nf < 4; ++nf) acc[nf][i] = multiply(w[nf], x[i], acc[nf][i]);
+        for (int i = 0; i < R; ++i) x[i] = row_codes(st0, i);
+        // `more`: stores that went out since the copies that are waited for
+        auto step = [&](auto what, auto more) __attribute__((always_inline)) {
+            constexpr int M = 4 * R, kFirst = R == 1 ? 0 : M / 2;       // from where on the next stage is read and copies go out
+            constexpr int F = decltype(what)::value, kEvery = R == 4 ? 2 : 1;   // row fragment of the unit before that is finished; pairs between its columns
+            f32x4 v[4][1], sw, bias = {0.f, 0.f, 0.f, 0.f};
+            float sx = 0.f;
+            if constexpr (F >= 0) {
+                sx = row_scale(done_place, F);
+                sw = *reinterpret_cast<const f32x4*>(columns_of(done_place));
+                if (a.bias != nullptr) bias = *reinterpret_cast<const f32x4*>(columns_of(done_place) + T::kBias - T::kSw);
+            }
             slot = slot == kStages - 1 ? 0 : slot + 1;
-        }
-        const int lane = here(threadIdx.x) & 63, r = lane & 15;
-        const int col0 = cur.group * kQuantBlock + wn * 64, first = wm * 16;            // this wavefront's columns and rows
-        const unsigned char* of = smem + T::kUnits + unit * T::kUnit;
-        const int at_columns = (wn * 64 + (lane >> 4) * 4) * 4;
-        float sx[R];
+            const unsigned char* st = smem + slot * kStage;
 #pragma unroll
-        for (int i = 0; i < R; ++i) sx[i] = *reinterpret_cast<const float*>(of + (first + i * 64 + r) * 4);
-        f32x4 v[4][R];
-        finish(a.act, sx, of + T::kSw + at_columns, a.bias != nullptr ? of + T::kBias + at_columns : nullptr, acc, v);
-        store_values<OUT, 64>(a, col0, cur.row0 + first, cur.rows - first, v);
+            for (int n = 0; n < M; ++n) {
+                const int half = n / (2 * R), i = n % (2 * R) >> 1, nf = 2 * half + (n & 1);
+                if (n == kFirst) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    copies_landed_unless<(kStages - 2) * T::kCopies + decltype(more)::value>(landed);
+                    landed = landed > 0 ? landed - 1 : 0;
+                    if (R > 1) {
+                        w[0] = weight_codes(st, 0);
+                        w[1] = weight_codes(st, 1);
+                    }
+                }
+                acc[nf][i] = multiply(w[nf], x[i], acc[nf][i]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (R == 1 && n < 2) w[n] = weight_codes(st, n);
+                if (half == 1 && i == R - 1) w[nf] = weight_codes(st, nf);
+                if (half == 1 && (n & 1)) x[i] = row_codes(st, i);
+                if constexpr (F >= 0) {
+                    if (n % kEvery == 0 && n / kEvery < 4) {
+                        const int c = n / kEvery;
+                        v[c][0] = finish_fragment<SMOOTH>(a.act, sx, sw, bias, old[c][F < 0 ? 0 : F]);
+                        if (c < 3) {
+                            sw = *reinterpret_cast<const f32x4*>(columns_of(done_place) + (c + 1) * 64);
+                            if (a.bias != nullptr) bias = *reinterpret_cast<const f32x4*>(columns_of(done_place) + T::kBias - T::kSw + (c + 1) * 64);
+                        }
+                    }
+                    if (n == (R == 1 ? 3 : M / 2)) store_all(done, F, v);
+                }
+                constexpr int kPer = (T::kCopies + M - kFirst - 1) / (M - kFirst);
+#pragma unroll
+                for (int c = 0; c < kPer; ++c)
+                    if (n >= kFirst) copy_piece((n - kFirst) * kPer + c);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto before_steps = [&]() __attribute__((always_inline)) {
+            // behind branches that not every lane takes, such as the stores of the unit before
+            u_in = uniform(u_in);
+            kb_in = uniform(kb_in);
+            slot_in = uniform(slot_in);
+            slot = uniform(slot);
+            landed = uniform(landed);
+            stage_step = uniform(stage_step);
+            weights_base = uniform(weights_base);
+            if constexpr (OFFSETS) rows_base = uniform(rows_base);
+            if (kb_in == KB) {
+                // Units of one step: the place that the next unit's scales go to is that of the unit before this one, which every wavefront
+                // has to be done with.  Longer units meet in their steps in between.
+                if (KB == 1) asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                next_unit();
+            }
+            // nothing pending on the way in (lgkmcnt(0), the compiler counts with it): the steps wait only for what they read themselves
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+        };
+        int j = 0;
+        if constexpr (R == RMAX) if (left) {
+            auto with_old = [&](auto f) __attribute__((always_inline)) {
+                before_steps();
+                step(f, std::integral_constant<int, 0>{});
+                next_stage();
+                ++kb_in;
+                before_steps();
+                step(std::integral_constant<int, -1>{}, std::integral_constant<int, R == 1 ? 0 : kStores>{});     // R == 1: they are behind the copies
+                next_stage();
+                ++kb_in;
+            };
+            with_old(std::integral_constant<int, 0>{});
+            if constexpr (R > 1) with_old(std::integral_constant<int, 1>{});
+            if constexpr (R > 2) {
+                with_old(std::integral_constant<int, 2>{});
+                with_old(std::integral_constant<int, 3>{});
+            }
+            left = false;
+            j = kSpread * R;
+        }
+        // the steps to the end of the unit or to where the copies go on to the next one: without a branch, so that the order stays
+#pragma unroll 1
+        while (j < KB) {
+            before_steps();
+            const int steps = min(KB - j, KB - kb_in);
+            j += steps;
+            kb_in += steps;
+#pragma unroll 1
+            for (int s = 0; s < steps; ++s) {
+                step(std::integral_constant<int, -1>{}, std::integral_constant<int, 0>{});
+                next_stage();
+            }
+        }
+        if constexpr (R == RMAX) {
+#pragma unroll
+            for (int nf = 0; nf < 4; ++nf)
+#pragma unroll
+                for (int i = 0; i < R; ++i) old[nf][i] = acc[nf][i];
+            done = cur;
+            done_place = unit;
+            left = true;
+        } else {
+            finish_now(cur, unit, acc, fragments);
+        }
         unit = unit == T::kPlaces - 1 ? 0 : unit + 1;
     };
+    auto all_fragments = [&](const Unit& w) { return RMAX == 1 || w.rows > 32 * RMAX; };
     while (true) {
-        if (RMAX == 1 || cur.rows <= 64) run_unit(std::integral_constant<int, 1>{});
-        else if (RMAX == 2 || cur.rows <= 128) run_unit(std::integral_constant<int, (RMAX < 2 ? RMAX : 2)>{});
-        else run_unit(std::integral_constant<int, RMAX>{});
+        if (all_fragments(cur)) run_unit(std::integral_constant<int, RMAX>{});
+        else if (RMAX < 4 || cur.rows <= 64) run_unit(std::integral_constant<int, (RMAX > 1 ? 1 : RMAX)>{});
+        else run_unit(std::integral_constant<int, (RMAX > 2 ? 2 : RMAX)>{});
         u = uniform(u + static_cast<int>(gridDim.x));
-        if (u >= units) break;
-        cur = unit_at(u);
+        const bool more = u < units;
+        if (more) cur = unit_at(u);
+        if (left && !(more && all_fragments(cur) && all_exist(done) && KB >= kSpread * RMAX)) {
+            finish_now(done, done_place, old, std::integral_constant<int, RMAX>{});
+            left = false;
+        }
+        if (!more) break;
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is used for something else by then
 }
 
 // Both kinds of units of a grouped product as one kernel, the tiles first: where one kind does not occur, a launch of its own would
 // cost 4 to 5 us all the same.  Streamed units are dealt from the last block number down, evenly over the XCDs.
-template <int OUT, int RMAX>
+template <int OUT, int RMAX, bool SMOOTH, bool PASS>
 __global__ __launch_bounds__(kTileWaves * 64) void int_product_kernel(const QuantArgs a, int tiled_min_rows) {
     extern __shared__ __align__(16) unsigned char smem[];
-    tile_units<OUT, RMAX>(a, tiled_min_rows, smem);
+    tile_units<OUT, RMAX, SMOOTH, PASS>(a, tiled_min_rows, smem);
     if (a.offsets == nullptr) return;
     __syncthreads();
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + kListAt);
     const int tiles = list_experts<kTileWaves * 64>(a, tiled_min_rows - 1, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
     const int b = gridDim.x - 1 - blockIdx.x;
-    if (tiles * quant_blocks(a.N) > static_cast<int>(gridDim.x)) stream_units<OUT, 2>(a, list, tiles, 1, b, smem);
-    else stream_units<OUT, 1>(a, list, tiles, 1, b, smem);
+    if (tiles * quant_blocks(a.N) > static_cast<int>(gridDim.x)) stream_units<OUT, 2, SMOOTH>(a, list, tiles, 1, b, smem);
+    else stream_units<OUT, 1, SMOOTH>(a, list, tiles, 1, b, smem);
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
@@ -517,7 +711,11 @@ int tile_fragments(int rows, int N, size_t operand_bytes) {
 template <int RMAX>
 constexpr int kProductLds = Tiles<RMAX>::kLdsBytes > kStreamLds ? Tiles<RMAX>::kLdsBytes : kStreamLds;
 
-template <int OUT>
+// Outputs that no L2 holds pass by it, so that the operands stay there: 16384 x 8192 x 2048, fp32 out (537 MB), 367 -> 333 us, bf16 342 -> 334; but 4096 x 4096 x
+// 1024, bf16 out (34 MB), 27.1 -> 28.2, 1501 x 1024 x 4096 (3 MB) 16.9 -> 17.8.
+constexpr size_t kCachedOutput = size_t{64} << 20;
+
+template <int OUT, bool SMOOTH>
 hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
     const int cus = device_cu_count();
     const dim3 grid(cus), threads(kStreamWaves * 64);
@@ -525,15 +723,17 @@ hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
     if (split > 1) {
         QuantArgs parts = a;
         parts.out = ws;
-        int_stream_kernel<kOutParts><<<grid, threads, kStreamLds, stream>>>(parts, a.rows, split);
-        int_join_kernel<OUT><<<dim3(a.rows, (a.N + 1023) / 1024), dim3(256), 0, stream>>>(a, static_cast<const int32_t*>(ws), split);
+        int_stream_kernel<kOutParts, false><<<grid, threads, kStreamLds, stream>>>(parts, a.rows, split);
+        int_join_kernel<OUT, SMOOTH><<<dim3(a.rows, (a.N + 1023) / 1024), dim3(256), 0, stream>>>(a, static_cast<const int32_t*>(ws), split);
     } else if (a.rows < kTiledMinRows) {
-        int_stream_kernel<OUT><<<grid, threads, kStreamLds, stream>>>(a, a.rows, 1);
+        int_stream_kernel<OUT, SMOOTH><<<grid, threads, kStreamLds, stream>>>(a, a.rows, 1);
     } else {
+        const size_t out_bytes = static_cast<size_t>(a.rows) * a.N * elem_size(a.out_dtype);
         const int r = tile_fragments(a.rows, a.N, a.rows / a.k * quant_pitch(a.K));
-        if (r == 4) int_product_kernel<OUT, 4><<<grid, threads, kProductLds<4>, stream>>>(a, kTiledMinRows);
-        else if (r == 2) int_product_kernel<OUT, 2><<<grid, threads, kProductLds<2>, stream>>>(a, kTiledMinRows);
-        else int_product_kernel<OUT, 1><<<grid, threads, kProductLds<1>, stream>>>(a, kTiledMinRows);
+        if (r == 4 && out_bytes > kCachedOutput) int_product_kernel<OUT, 4, SMOOTH, true><<<grid, threads, kProductLds<4>, stream>>>(a, kTiledMinRows);
+        else if (r == 4) int_product_kernel<OUT, 4, SMOOTH, false><<<grid, threads, kProductLds<4>, stream>>>(a, kTiledMinRows);
+        else if (r == 2) int_product_kernel<OUT, 2, SMOOTH, false><<<grid, threads, kProductLds<2>, stream>>>(a, kTiledMinRows);
+        else int_product_kernel<OUT, 1, SMOOTH, false><<<grid, threads, kProductLds<1>, stream>>>(a, kTiledMinRows);
     }
     return hipGetLastError();
 }
@@ -541,13 +741,14 @@ hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
 hipError_t allow_lds(const void* kernel, int bytes) {
     return hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
 }
-template <int OUT>
+template <int OUT, bool SMOOTH>
 hipError_t configure_out() {
     hipError_t e;
-    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 4>), kProductLds<4>)) != hipSuccess) return e;
-    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 2>), kProductLds<2>)) != hipSuccess) return e;
-    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 1>), kProductLds<1>)) != hipSuccess) return e;
-    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<OUT>), kStreamLds);
+    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 4, SMOOTH, true>), kProductLds<4>)) != hipSuccess) return e;
+    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 4, SMOOTH, false>), kProductLds<4>)) != hipSuccess) return e;
+    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 2, SMOOTH, false>), kProductLds<2>)) != hipSuccess) return e;
+    if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 1, SMOOTH, false>), kProductLds<1>)) != hipSuccess) return e;
+    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<OUT, SMOOTH>), kStreamLds);
 }
 
 // Weights that do not fit the L2s (8 x 4 MiB) are gone before the next call reads them, or have pushed out the rows: streamed units then read
@@ -564,15 +765,18 @@ size_t int_product_workspace(const moe_quant_shape& s) {
 
 hipError_t configure_int_kernels() {
     hipError_t e;
-    if ((e = configure_out<kOutF32>()) != hipSuccess) return e;
-    if ((e = configure_out<kOutBf16>()) != hipSuccess) return e;
-    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<kOutParts>), kStreamLds);
+    if ((e = configure_out<kOutF32, false>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutF32, true>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutBf16, false>()) != hipSuccess) return e;
+    if ((e = configure_out<kOutBf16, true>()) != hipSuccess) return e;
+    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<kOutParts, false>), kStreamLds);
 }
 
 hipError_t launch_int_product(const QuantArgs& args, void* ws, hipStream_t stream) {
     QuantArgs a = args;
     a.once = a.E * quant_matrix_bytes(a.N, a.K) > kCachedWeights;
-    return a.out_dtype == MOE_F32 ? launch_out<kOutF32>(a, ws, stream) : launch_out<kOutBf16>(a, ws, stream);
+    if (is_smooth(a.act)) return a.out_dtype == MOE_F32 ? launch_out<kOutF32, true>(a, ws, stream) : launch_out<kOutBf16, true>(a, ws, stream);
+    return a.out_dtype == MOE_F32 ? launch_out<kOutF32, false>(a, ws, stream) : launch_out<kOutBf16, false>(a, ws, stream);
 }
 
 }  // namespace moe
