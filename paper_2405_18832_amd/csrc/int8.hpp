@@ -38,8 +38,9 @@ struct IntRowArgs {
 
 // csrc/int_rows.hip
 hipError_t launch_norm_quantize_int(const IntRowArgs& a, int dtype, hipStream_t stream);
-hipError_t launch_act_quantize_int(const IntRowArgs& a, int dtype, hipStream_t stream);
 hipError_t launch_quantize_weights_int(int E, int N, int K, int src_dtype, const void* src, uint8_t* dst, float* scales, hipStream_t stream);
+// csrc/int_act.hip
+hipError_t launch_act_quantize_int(const IntRowArgs& a, int dtype, hipStream_t stream);
 // csrc/int_linear.hip
 size_t int_product_workspace(const moe_quant_shape& s);
 hipError_t launch_int_product(const QuantArgs& a, void* ws, hipStream_t stream);

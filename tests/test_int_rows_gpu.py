@@ -1,7 +1,7 @@
 """int8 rows and weights against the 64-bit reference (oracle/int_oracle.py).
 
 Codes are the definition's whole numbers, so they are equal.  Scales, u = 2^-24 (half a step of fp32): the largest magnitude rounded to fp32 and divided,
-2 u; the norm's factor on top, a sum of d squares in chains of 8, of the chunks that a lane keeps and of the lanes (d <= 20000: 8 + 8 + 6 + 8
+2 u (with none or ReLU, gated: 3 u); behind GeLU and SiLU it may be the fp32 activation's, which is taken where its error is below 2^-17 of itself; the norm's factor on top, a sum of d squares in chains of 8, of the chunks that a lane keeps and of the lanes (d <= 20000: 8 + 8 + 6 + 8
 additions, halved by the square root), mean, eps, root and quotient: 24 u together.  NORM = 3e-6 covers 50 u; the norm's two products are in it.
 """
 import sys
@@ -150,7 +150,7 @@ def act_case(moe, h, act, gated, dtype, offsets=None, mask=None, offset=0):
     idle = torch.from_numpy(np.concatenate([~run, [True]])).cuda()
     assert (q[idle] == 77).all() and (s[idle] == 77).all()      # other rows are left as they were
     at = torch.from_numpy(np.flatnonzero(run)).cuda()
-    check_rows(q[at], s[at], v[run], None, 2.0 ** -22, f)
+    check_rows(q[at], s[at], v[run], None, 2.0 ** -17 if act in ("gelu", "silu") else 2.0 ** -22, f)
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
