@@ -240,6 +240,35 @@ __device__ __forceinline__ V wave_reduce(V v, Op op) {
     return op(op(lane_of(v, 0), lane_of(v, 16)), op(lane_of(v, 32), lane_of(v, 48)));
 }
 
+// The groups that stay, from a token's choices `row` [E], by a wavefront.
+__device__ __forceinline__ uint64_t groups_that_stay(const ScoreArgs& a, const double* row, double* group, int lane, int size) {
+    double mine = kNone;
+    if (lane < a.groups) {
+        double first = kNone, second = kNone;
+#pragma unroll 8
+        for (int i = 0; i < size; ++i) {
+            const double c = row[lane * size + i];
+            second = fmax(second, fmin(first, c));
+            first = fmax(first, c);
+        }
+        mine = a.top == 2 ? first + second : first;
+        group[lane] = mine;
+    }
+    __builtin_amdgcn_wave_barrier();
+    int ahead = 0;
+    if (lane < a.groups)
+#pragma unroll 8
+        for (int o = 0; o < a.groups; ++o) ahead += group[o] > mine || (group[o] == mine && o < lane) ? 1 : 0;
+    return __ballot(lane < a.groups && ahead < a.kept);
+}
+// The same for finite logits and sigmoid scores.
+__device__ __forceinline__ uint64_t groups_that_stay(const ScoreArgs& a, double* row, const float* values, double* group, int lane, int E) {
+#pragma unroll 2
+    for (int e = lane; e < E; e += 64) row[e] = 1.0 / (1.0 + exp(-static_cast<double>(values[e]))) + (a.balance != nullptr ? static_cast<double>(a.balance[e]) : 0.0);
+    __builtin_amdgcn_wave_barrier();
+    return groups_that_stay(a, row, group, lane, E / a.groups);
+}
+
 // One token's experts and weights, by a wavefront, in 64 bits.  `row` [E], `values` [E] (the logits, if they are `loaded`) and
 // `group` [groups]: LDS.
 __device__ __forceinline__ void choose_exactly(const ScoreArgs& a, double* row, float* values, bool loaded, double* group, int lane, long t, int32_t* hist) {
@@ -283,23 +312,7 @@ __device__ __forceinline__ void choose_exactly(const ScoreArgs& a, double* row, 
     }
     __builtin_amdgcn_wave_barrier();
     if (a.groups > 1) {
-        double mine = kNone;
-        if (lane < a.groups) {
-            double first = kNone, second = kNone;
-#pragma unroll 8
-            for (int i = 0; i < size; ++i) {
-                const double c = row[lane * size + i];
-                second = fmax(second, fmin(first, c));
-                first = fmax(first, c);
-            }
-            mine = a.top == 2 ? first + second : first;
-            group[lane] = mine;
-        }
-        __builtin_amdgcn_wave_barrier();
-        int ahead = 0;
-        if (lane < a.groups)
-            for (int o = 0; o < a.groups; ++o) ahead += group[o] > mine || (group[o] == mine && o < lane) ? 1 : 0;
-        const uint64_t stay = __ballot(lane < a.groups && ahead < a.kept);
+        const uint64_t stay = groups_that_stay(a, row, group, lane, size);
 #pragma unroll 1
         for (int e = lane; e < E; e += 64) {
             const float l = values[e];
@@ -485,14 +498,23 @@ __device__ __forceinline__ void largest_eight(int* v) {
     }
 }
 
+// Bytes of LDS of a wavefront: rows of four tokens' choices in fp32 or of one token's in 64 bits, rows of four tokens' logits, and the groups'.
+__host__ __device__ constexpr int score_row_bytes(int E) { return 16 * E; }
+__host__ __device__ constexpr int score_wave_bytes(int E) { return 2 * score_row_bytes(E) + MOE_MAX_GROUPS * 8; }
+
 constexpr int kFastGroups = 16;
 template <int V, bool SIGMOID, bool BALANCED>
-__device__ __forceinline__ bool choose(const ScoreArgs& a, float* row, float* values, float* group, int sub, bool live, long t, long last, int32_t* hist) {
+__device__ __forceinline__ bool choose(const ScoreArgs& a, unsigned char* lds, int lane, bool live, long t, long last, int32_t* hist) {
     constexpr float kLog2e = 1.4426950408889634f;
     constexpr int kKept = V < 8 ? V : 8;
     // what follows from these is computed where it is used: kept from one turn of the caller's loop to the next, it would need 100 registers more
-    int E = a.E, base = 4 * sub;
-    asm volatile("" : "+s"(E), "+v"(base));
+    int E = a.E, sub = lane & 15;
+    asm volatile("" : "+s"(E), "+v"(sub));
+    const int base = 4 * sub, slot = lane >> 4;
+    float* row = reinterpret_cast<float*>(lds) + slot * E;
+    float* all_values = reinterpret_cast<float*>(lds + score_row_bytes(E));
+    float* values = all_values + slot * E;
+    float* group = reinterpret_cast<float*>(lds + 2 * score_row_bytes(E)) + slot * kFastGroups;
     const long from = min(t, last - 1) * E;
     float c[V];
     if (a.bf16) load_row(static_cast<const uint16_t*>(a.logits) + from, E, base, c);
@@ -580,11 +602,26 @@ __device__ __forceinline__ bool choose(const ScoreArgs& a, float* row, float* va
             const float v = group[o];
             ahead += v > mine || (v == mine && o < g) ? 1 : 0;
         }
-        const bool stays = g < a.groups && ahead < a.kept;
+        bool stays = g < a.groups && ahead < a.kept;
         if (BALANCED || by_score) {
             const float low = unordered(least_of(ordered(stays ? mine : -kLow)));
             const float high = unordered(most_of(ordered(g < a.groups && !stays ? mine : kLow)));
-            unsure |= !(low - high > 2.f * doubt<SIGMOID>(low));     // sums of two
+            const bool close = !(low - high > 2.f * doubt<SIGMOID>(low));        // sums of two
+            if (SIGMOID) {                     // 64 bits say which groups stay, a token at a time
+                __builtin_amdgcn_wave_barrier();
+                uint64_t left = __ballot(close && live && sub == 0);
+#pragma unroll 1
+                while (left != 0) {
+                    const int n = __builtin_ctzll(left) >> 4;
+                    left &= left - 1;
+                    const uint64_t exact = groups_that_stay(a, reinterpret_cast<double*>(lds), all_values + n * E,
+                                                            reinterpret_cast<double*>(lds + 2 * score_row_bytes(E)), lane, E);
+                    if (slot == n) stays = (exact >> g & 1) != 0;
+                    __builtin_amdgcn_wave_barrier();
+                }
+            } else {
+                unsure |= close;
+            }
         }
         const uint32_t stay = static_cast<uint32_t>(__ballot(stays) >> (threadIdx.x & 48)) & 0xffffu;
         const uint32_t inverse = ((1u << 20) + size - 1) / size;            // e * inverse >> 20 = e / size for e, size <= 1024
@@ -629,7 +666,11 @@ __device__ __forceinline__ bool choose(const ScoreArgs& a, float* row, float* va
     largest_eight<V>(n);
     int mine = 0, taken = 0;                                    // lane j keeps the winner of round j; how many of the lane's have won
     float before = -kLow;
-    const int rounds = numbered ? a.k : min(a.k + 1, a.kept * (E / a.groups));      // one more says whether the last was beyond doubt
+    // One more says whether the last was beyond doubt.  Sigmoid: two more; if the best k or k + 1 are, as a set, their order may be in doubt and is settled in 64 bits
+    // below (nine differences in doubt once in 250 tokens of 256 experts, two next to each other hardly ever).
+    constexpr bool kSettled = SIGMOID && BALANCED;
+    const int rounds = numbered ? a.k : min(a.k + (kSettled ? 2 : 1), a.kept * (E / a.groups));
+    bool in_order = true, best_k = true, best_k1 = true;
 #pragma unroll 1
     for (int j = 0; j < rounds; ++j) {
         const int best = most_of(n[0]), q = V - 1 - (best & (V - 1));
@@ -641,12 +682,36 @@ __device__ __forceinline__ bool choose(const ScoreArgs& a, float* row, float* va
         if (won) n[kKept - 1] = -0x7fffffff - 1;
         taken += won ? 1 : 0;
         const float value = BALANCED ? static_cast<float>(best / V) * kUnit : unordered(best);
-        if (BALANCED) unsure |= !(before - value > doubt<SIGMOID>(value) + 3.f * kUnit) || !(value > 1.f - kFar);
-        else if (!numbered) unsure |= !(before - value > fmaf(fabsf(value), V * 0x1p-23f, V * 0x1p-126f));
+        if (BALANCED) {
+            const bool apart = before - value > doubt<SIGMOID>(value) + 3.f * kUnit && value > 1.f - kFar;
+            if (!kSettled) unsure |= !apart;
+            else if (j < a.k) in_order &= apart;
+            else if (j == a.k) best_k = apart;
+            else best_k1 = apart;
+        } else if (!numbered) unsure |= !(before - value > fmaf(fabsf(value), V * 0x1p-23f, V * 0x1p-126f));
         before = value;
         if (sub == j) mine = min(at, E - 1);
     }
     __builtin_amdgcn_wave_barrier();
+    if (kSettled) {
+        unsure |= !best_k && !best_k1;
+        const bool settle = !in_order || !best_k;
+        if (__ballot(settle) != 0) {
+            const int m = best_k ? a.k : a.k + 1;
+            const double c = sub < m ? 1.0 / (1.0 + exp(-static_cast<double>(values[mine]))) + static_cast<double>(a.balance[mine]) : kNone;
+            int place = 0, settled = mine;
+            for (int i = 0; i <= a.k; ++i) {
+                const double other = __shfl(c, i, 16);
+                const int e = __shfl(mine, i, 16);
+                place += i < m && (other > c || (other == c && e < mine)) ? 1 : 0;
+            }
+            for (int i = 0; i <= a.k; ++i) {
+                const int to = __shfl(place, i, 16), e = __shfl(mine, i, 16);
+                settled = i < m && to == sub ? e : settled;
+            }
+            if (settle) mine = settled;
+        }
+    }
     unsure |= V > 8 && taken >= 8;                              // what comes next in the lane is not known
     float p = 1.f;
     if (sub < a.k) {
@@ -690,10 +755,6 @@ __device__ __forceinline__ void finish_counts(const ScoreArgs& a, int mine, int3
     }
 }
 
-// Bytes of LDS of a wavefront: rows of four tokens' choices in fp32 or of one token's in 64 bits, rows of four tokens' logits, and the groups'.
-__host__ __device__ constexpr int score_row_bytes(int E) { return 16 * E; }
-__host__ __device__ constexpr int score_wave_bytes(int E) { return 2 * score_row_bytes(E) + MOE_MAX_GROUPS * 8; }
-
 // A block takes `tokens` tokens, 4 per wavefront at a time.  ONE: it is the only block and goes on to the outputs of the
 // counts; else its counts go to the workspace, [block][E] of 16 bits.
 template <int V>
@@ -717,8 +778,7 @@ __global__ __launch_bounds__(kRouteScoreWaves<V> * 64) void route_scores_kernel(
         const bool live = t < last;
         bool sure = false;
         if (a.groups <= kFastGroups)
-            sure = choose<V, SIGMOID, BALANCED>(a, reinterpret_cast<float*>(mine) + slot * a.E, values + slot * a.E, reinterpret_cast<float*>(group) + slot * 16,
-                                                lane & 15, live, t, last, hist);
+            sure = choose<V, SIGMOID, BALANCED>(a, mine, lane, live, t, last, hist);
         uint64_t left = __ballot(!sure && live && (lane & 15) == 0);
 #pragma unroll 1
         while (left != 0) {
