@@ -57,8 +57,9 @@ def activate(v: np.ndarray, act: str) -> np.ndarray:
 
 
 def product(a, sa, w, sw, bias=None):
-    """(sa sw a w^T + bias, |sa sw a w^T|): before the activation, and what the errors of its scales are relative to."""
-    z = (a.astype(np.int64) @ w.astype(np.int64).T).astype(np.float64) * np.asarray(sa, dtype=np.float64)[:, None] * np.asarray(sw, dtype=np.float64)[None]
+    """(sa sw a w^T + bias, |sa sw a w^T|): before the activation, and what the errors of its scales are relative to.  The sums of whole numbers are
+    exact: they stay below 2^53."""
+    z = (a.astype(np.float64) @ w.astype(np.float64).T) * np.asarray(sa, dtype=np.float64)[:, None] * np.asarray(sw, dtype=np.float64)[None]
     return (z if bias is None else z + np.asarray(bias, dtype=np.float64)), np.abs(z)
 
 

@@ -73,7 +73,7 @@ struct Streams {
 constexpr int kOutParts = 3;
 
 template <int OUT, int NF, bool SMOOTH>
-__device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t* list, int tiles, int parts_wanted, int b, unsigned char* smem) {
+__device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t* list, int tiles, int parts_wanted, int b, int G, unsigned char* smem) {
     using S = Streams<NF>;
     constexpr int kStages = S::kStages, kStage = S::kStage;
     const int split = OUT == kOutParts ? parts_wanted : 1;
@@ -82,9 +82,9 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
     const int per_tile = groups * split, units = tiles * per_tile;
 
-    // Every block gets the same number of units, as few as the grid allows: a CU can pull more than its share of the memory's rate, so
+    // Block b of G.  Every block gets the same number of units, as few as the grid allows: a CU can pull more than its share of the memory's rate, so
     // that a quarter of them idle costs nothing, but a last round of a few units does.  The runs are dealt to the XCDs evenly.
-    const int G = gridDim.x, rounds = (units + G - 1) / G, runs = rounds > 0 ? (units + rounds - 1) / rounds : 0;
+    const int rounds = (units + G - 1) / G, runs = rounds > 0 ? (units + rounds - 1) / rounds : 0;
     const int per_xcd = (runs + 7) >> 3;
     const int run = G % 8 == 0 ? (b >> 3 < per_xcd ? (b & 7) * per_xcd + (b >> 3) : runs) : b;
     const int first = run * rounds, last = min(units, first + rounds);
@@ -262,7 +262,7 @@ __global__ __launch_bounds__(kStreamWaves * 64) void int_stream_kernel(const Qua
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + kListAt);
     const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
-    stream_units<OUT, 1, SMOOTH>(a, list, tiles, parts_wanted, blockIdx.x, smem);
+    stream_units<OUT, 1, SMOOTH>(a, list, tiles, parts_wanted, blockIdx.x, gridDim.x, smem);
 }
 
 // Adds up the parts of a split contraction and finishes the rows.  A block of threads per row and 1024 columns, four per thread.
@@ -314,21 +314,82 @@ struct Tiles {
     static_assert(kLdsBytes <= 160 * 1024, "fits a CU");
 };
 
+// What there is to do of a grouped product, counted by every block for itself (a list in memory would cost a launch): experts of at least min_rows rows run in
+// tiles of tile_rows rows.  whole[e] is the number of whole tiles that the experts before e have, whole[E] that of all (at most as many as the rows have, so
+// that offsets that are none do not overflow what follows); `rest` lists the experts with a shorter last tile, those of more than 128 rows first, then of more
+// than 64, then the others.  `tmp`: four ints per wavefront.  One matrix: all rows are its.
+struct Work {
+    int whole, last[3], streamed;          // tiles; last tiles by length; experts of fewer rows
+};
+template <int THREADS>
+__device__ __forceinline__ Work count_work(const QuantArgs& a, int tile_rows, int min_rows, int32_t* whole, uint16_t* rest, int4* tmp) {
+    constexpr int W = THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, most = a.rows / tile_rows;
+    const int least = a.offsets == nullptr ? 1 : min_rows;
+    int4 before = {0, 0, 0, 0};            // whole tiles; last tiles by length, streamed experts: 16 bits each hold 1024
+    int base1 = 0, base2 = 0;
+    // the lengths' totals are needed before the first expert's place is known: first pass counts, second one places
+    for (int pass = 0; pass < 2; ++pass) {
+        if (pass == 1) {
+            base1 = before.y & 0xffff;
+            base2 = base1 + (before.y >> 16);
+            if (threadIdx.x == 0) whole[a.E] = before.x;
+            before = int4{0, 0, 0, 0};
+        }
+        for (int e0 = 0; e0 < a.E; e0 += THREADS) {
+            const int e = e0 + threadIdx.x;
+            const int rows = e < a.E ? segment_of(a, e).rows : 0, m = rows < least ? 0 : rows;
+            const int n = m / tile_rows, left = m - n * tile_rows;
+            const int kind = left == 0 ? -1 : left > 128 ? 0 : left > 64 ? 1 : 2;
+            const int incl = wave_scan(n);
+            const uint64_t k0 = __ballot(kind == 0), k1 = __ballot(kind == 1), k2 = __ballot(kind == 2), few = __ballot(rows > 0 && m == 0);
+            if (lane == 63) tmp[wave] = int4{incl, __popcll(k0) | __popcll(k1) << 16, __popcll(k2) | __popcll(few) << 16, 0};
+            __syncthreads();
+            int4 mine = before;
+            for (int w = 0; w < W; ++w) {
+                const int4 t = tmp[w];
+                if (w < wave) mine = int4{min(mine.x + t.x, most), mine.y + t.y, mine.z + t.z, 0};
+                before = int4{min(before.x + t.x, most), before.y + t.y, before.z + t.z, 0};
+            }
+            if (pass == 1) {
+                if (e < a.E) whole[e] = min(mine.x + incl - n, most);
+                const uint64_t below = (1ull << lane) - 1;
+                const int at = kind == 0 ? (mine.y & 0xffff) + __popcll(k0 & below)
+                             : kind == 1 ? base1 + (mine.y >> 16) + __popcll(k1 & below)
+                                         : base2 + (mine.z & 0xffff) + __popcll(k2 & below);
+                if (kind >= 0) rest[at] = static_cast<uint16_t>(e);
+            }
+            __syncthreads();
+        }
+    }
+    return Work{uniform(before.x), {uniform(before.y & 0xffff), uniform(before.y >> 16), uniform(before.z & 0xffff)}, uniform(before.z >> 16)};
+}
+
+template <int RMAX>
+__device__ __forceinline__ int32_t* tile_starts(unsigned char* smem) {
+    return reinterpret_cast<int32_t*>(smem + Tiles<RMAX>::kStarts + kTileWaves * 16);
+}
+template <int RMAX>
+__device__ __forceinline__ Work count_work(const QuantArgs& a, int min_rows, unsigned char* smem) {
+    int32_t* whole = tile_starts<RMAX>(smem);
+    return count_work<kTileWaves * 64>(a, Tiles<RMAX>::kRows, min_rows, whole, reinterpret_cast<uint16_t*>(whole + MOE_MAX_E + 1),
+                                       reinterpret_cast<int4*>(smem + Tiles<RMAX>::kStarts));
+}
+
+// Units first, first + stride, ... before `end`, of the whole tiles' and then the last tiles' (see count_work, which has left their lists).
 // PASS: the output passes by the caches.
 template <int OUT, int RMAX, bool SMOOTH, bool PASS>
-__device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, unsigned char* smem) {
+__device__ __forceinline__ void tile_units(const QuantArgs& a, int whole_tiles, int first, int end, int stride, unsigned char* smem) {
     using T = Tiles<RMAX>;
     constexpr int kStages = T::kStages, kStageW = T::kStageW, kStage = T::kStage, tile_rows = T::kRows;
-    int4* counts = reinterpret_cast<int4*>(smem + T::kStarts);
-    int32_t* whole = reinterpret_cast<int32_t*>(counts + kTileWaves);
-    uint16_t* rest = reinterpret_cast<uint16_t*>(whole + MOE_MAX_E + 1);
-    const int last_tiles = count_tiles<kTileWaves * 64>(a, tile_rows, min_rows, whole, rest, counts);
+    const int32_t* whole = tile_starts<RMAX>(smem);
+    const uint16_t* rest = reinterpret_cast<const uint16_t*>(whole + MOE_MAX_E + 1);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
     const int wm = wave >> 1, wn = wave & 1;
     const int KB = quant_blocks(a.K), groups = quant_blocks(a.N);
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
-    const int whole_units = __builtin_amdgcn_readfirstlane(whole[a.E]) * groups, units = whole_units + last_tiles * groups;
-    int u = xcd_position(), u_in = u;       // the unit that is computed, and the one that is copied
+    const int whole_units = whole_tiles * groups, units = end;
+    int u = first, u_in = u;                // the unit that is computed, and the one that is copied
     if (u >= units) return;
 
     struct Unit {
@@ -418,8 +479,8 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
     // when all of a unit's stages have been sent for (kb_in == KB)
     auto next_unit = [&]() __attribute__((always_inline)) {
         kb_in = 0;
-        if (u_in + static_cast<int>(gridDim.x) < units) {
-            u_in += gridDim.x;
+        if (u_in + stride < units) {
+            u_in += stride;
             ahead = unit_at(u_in);
             point_at(ahead);
         } else if (stage_step != 0) {      // back to the last stage, which is copied from now on
@@ -657,7 +718,7 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
         if (all_fragments(cur)) run_unit(std::integral_constant<int, RMAX>{});
         else if (RMAX < 4 || cur.rows <= 64) run_unit(std::integral_constant<int, (RMAX > 1 ? 1 : RMAX)>{});
         else run_unit(std::integral_constant<int, (RMAX > 2 ? 2 : RMAX)>{});
-        u = uniform(u + static_cast<int>(gridDim.x));
+        u = uniform(u + stride);
         const bool more = u < units;
         if (more) cur = unit_at(u);
         if (left && !(more && all_fragments(cur) && all_exist(done) && KB >= kSpread * RMAX)) {
@@ -669,19 +730,55 @@ __device__ __forceinline__ void tile_units(const QuantArgs& a, int min_rows, uns
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is used for something else by then
 }
 
-// Both kinds of units of a grouped product as one kernel, the tiles first: where one kind does not occur, a launch of its own would
-// cost 4 to 5 us all the same.  Streamed units are dealt from the last block number down, evenly over the XCDs.
+// All of a grouped product as one kernel: where one kind of unit does not occur, a launch of its own would cost 4 to 5 us all the same.
+// Long tiles are bound by the matrix units, short last tiles and streamed experts by memory, of which a CU alone gets 35 GB/s and 256 of them 20 each.  So
+// where there are rounds of the former, some CUs of every XCD (as many as the two kinds' times give, see memory_blocks) do the latter while the others
+// do the tiles; else all do the tiles first, then the streamed units, which are dealt from the last block number down.
+template <int RMAX>
+__device__ __forceinline__ int memory_blocks(int grid, int long_units, int short_units, int streamed_units) {       // a multiple of 8
+    if (grid % 8 != 0 || long_units < grid) return 0;
+    // us per step: of a long tile where the others do something else, of what a CU takes from memory
+    const float l = long_units * (RMAX == 4 ? 1.1f : RMAX == 2 ? 0.7f : 0.6f), m = short_units * 0.6f + streamed_units * 0.5f;
+    const int per_xcd = grid / 8, n = static_cast<int>(static_cast<float>(per_xcd) * m / (l + m) + 0.5f);
+    return 8 * min(n, per_xcd - 1);
+}
 template <int OUT, int RMAX, bool SMOOTH, bool PASS>
 __global__ __launch_bounds__(kTileWaves * 64) void int_product_kernel(const QuantArgs a, int tiled_min_rows) {
     extern __shared__ __align__(16) unsigned char smem[];
-    tile_units<OUT, RMAX, SMOOTH, PASS>(a, tiled_min_rows, smem);
-    if (a.offsets == nullptr) return;
-    __syncthreads();
-    uint16_t* list = reinterpret_cast<uint16_t*>(smem + kListAt);
-    const int tiles = list_experts<kTileWaves * 64>(a, tiled_min_rows - 1, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
-    const int b = gridDim.x - 1 - blockIdx.x;
-    if (tiles * quant_blocks(a.N) > static_cast<int>(gridDim.x)) stream_units<OUT, 2, SMOOTH>(a, list, tiles, 1, b, smem);
-    else stream_units<OUT, 1, SMOOTH>(a, list, tiles, 1, b, smem);
+    const int groups = quant_blocks(a.N), grid = gridDim.x, at = xcd_position();
+    Work work = count_work<RMAX>(a, tiled_min_rows, smem);
+    const int long_units = (work.whole + work.last[0]) * groups, units = long_units + (work.last[1] + work.last[2]) * groups;
+    const int streamed = work.streamed * groups, apart = uniform(memory_blocks<RMAX>(grid, long_units, units - long_units, streamed));
+    auto stream = [&](int b, int blocks) __attribute__((always_inline)) {
+        uint16_t* list = reinterpret_cast<uint16_t*>(smem + kListAt);
+        const int tiles = list_experts<kTileWaves * 64>(a, tiled_min_rows - 1, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
+        // Units of 256 columns read each row fragment for twice the columns; but where those of 128 are at most one per block they use more of the CUs.
+        if (tiles * groups > blocks) stream_units<OUT, 2, SMOOTH>(a, list, tiles, 1, b, blocks, smem);
+        else stream_units<OUT, 1, SMOOTH>(a, list, tiles, 1, b, blocks, smem);
+    };
+    int first = at, end = units, stride = grid;
+    if (apart != 0) {
+        const int per_xcd = grid / 8, mine = per_xcd - apart / 8, xcd = at / per_xcd, n = at - xcd * per_xcd;
+        if (n < mine) {
+            first = xcd * mine + n;
+            end = long_units;
+            stride = 8 * mine;
+        } else {
+            if (streamed > 0) {
+                __syncthreads();               // everybody has read the counts
+                stream((n - mine) * 8 + xcd, apart);
+                __syncthreads();
+                work = count_work<RMAX>(a, tiled_min_rows, smem);
+            }
+            first = long_units + xcd * (apart / 8) + n - mine;
+            stride = apart;
+        }
+    }
+    tile_units<OUT, RMAX, SMOOTH, PASS>(a, work.whole, uniform(first), uniform(end), uniform(stride), smem);
+    if (apart == 0 && streamed > 0) {
+        __syncthreads();
+        stream(grid - 1 - static_cast<int>(blockIdx.x), grid);
+    }
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------

@@ -152,6 +152,21 @@ def test_experts(gpu_lib, sizes, k, N, K, masked, out):
     p.experts(sizes, 1, "relu", False, out, gather=False, mask=mask)
 
 
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("sizes,N,K", [
+    ([4000, 5000, 100, 3, 64, 120, 0, 65, 1, 30], 1024, 300), ([9000, 0, 0, 0], 1100, 128), ([8500] + [7, 0, 90] * 60, 1024, 384), ([5000, 5000, 128, 127], 1024, 1100),
+    ([3000, 1] * 2 + [66] * 9, 3000, 200), ([2, 9100, 60], 1024, 130), ([1500] * 5 + [5] * 5, 1300, 520),
+])
+def test_experts_side_by_side(gpu_lib, sizes, N, K, masked, out):
+    """A round of long tiles and more, which some of the CUs leave to the others while they do what memory bounds; sums of one to nine blocks."""
+    say(f"[case] int experts side by side {sum(sizes)} rows of {len(sizes)} x {N} x {K} masked {masked} {out}")
+    behind = (-sum(sizes)) % 2
+    p = Problem(gpu_lib, sum(sizes) + behind, N, K, len(sizes))
+    mask = (np.random.default_rng(3).random(len(sizes)) < 0.8).astype(np.uint8) if masked else None
+    p.experts(sizes, 2, "gelu" if masked else "relu", True, out, mask=mask, behind=behind)
+
+
 @pytest.mark.parametrize("sizes,N,K", [([0] * 7 + [64] + [0] * 20 + [3, 1] + [0] * 10, 1024, 1024), ([0] * 39 + [9], 1024, 1024), ([1, 0, 40], 4000, 4096)])
 def test_weights_that_no_cache_holds(gpu_lib, sizes, N, K):
     say(f"[case] int weights read once {sum(sizes)} rows of {len(sizes)} x {N} x {K}")
