@@ -180,18 +180,26 @@ void launch_rows(Kernel kernel, const IntRowArgs& a, hipStream_t stream) {
     kernel<<<dim3(std::min(blocks, kAcross), (blocks + kAcross - 1) / kAcross), dim3(WAVES * 64), 0, stream>>>(a);
 }
 
-// go(WPR, WAVES, NV): a row of up to four chunks is one wavefront's where there are rows enough for all CUs, longer ones are shared out.
+// go(WPR, WAVES, NV): as many wavefronts per row as keep busy; where there are rows enough for all CUs, longer rows are left to fewer (GB/s, gated SiLU in
+// bf16, one wavefront per row, four with a chunk each, four chunks each, sixteen: 20000 x 700 2500, 1660, -, -; 20011 x 2048 4100, 4700, -, -; 8000 x 4096 -, -,
+// 4900, 3100; 8000 x 8192 -, -, 4500, 3900).
 constexpr int kFewRows = 1024;
+template <int WPR, int WAVES, int NV, typename Go>
+void row_variant(Go go) {
+    go(std::integral_constant<int, WPR>{}, std::integral_constant<int, WAVES>{}, std::integral_constant<int, NV>{});
+}
 template <typename Go>
 void with_row_variant(const IntRowArgs& a, Go go) {
     const int chunks = (a.d + kChunk - 1) / kChunk;
-    using std::integral_constant;
-    if (chunks <= 4 && a.rows >= kFewRows) go(integral_constant<int, 1>{}, integral_constant<int, 4>{}, integral_constant<int, 4>{});
-    else if (chunks <= 4) go(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 1>{});
-    else if (chunks <= 16 && a.rows >= kFewRows) go(integral_constant<int, 4>{}, integral_constant<int, 4>{}, integral_constant<int, 4>{});
-    else if (chunks <= 16) go(integral_constant<int, 16>{}, integral_constant<int, 16>{}, integral_constant<int, 1>{});
-    else if (chunks <= 64) go(integral_constant<int, 16>{}, integral_constant<int, 16>{}, integral_constant<int, 4>{});
-    else go(integral_constant<int, 16>{}, integral_constant<int, 16>{}, integral_constant<int, 0>{});
+    const bool many = a.rows >= kFewRows;
+    if (chunks <= 2 && many) row_variant<1, 4, 2>(go);
+    else if (chunks <= 4) row_variant<4, 4, 1>(go);
+    else if (chunks <= 8 && many) row_variant<4, 4, 2>(go);
+    else if (chunks <= 16 && many) row_variant<4, 4, 4>(go);
+    else if (chunks <= 16) row_variant<16, 16, 1>(go);
+    else if (chunks <= 32 && many) row_variant<8, 8, 4>(go);
+    else if (chunks <= 64) row_variant<16, 16, 4>(go);
+    else row_variant<16, 16, 0>(go);
 }
 
 }  // namespace
