@@ -50,7 +50,7 @@ __device__ __forceinline__ typename Piece<ST>::type load_piece(const ST* row, in
 }
 
 // 16 tokens x 16 experts per block; its wavefronts take shares of the contraction, which are added up in their order.
-constexpr int kGateWaves = 16, kGateFewBlocks = 256;
+constexpr int kGateWaves = 16;
 template <typename ST>
 __global__ __launch_bounds__(kGateWaves * 64) void gate_few_kernel(const ST* __restrict__ x, const ST* __restrict__ wg, const float* __restrict__ bias,
                                                                    float* __restrict__ logits, int T, int d, int E) {
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kGateWaves * 64) void gate_few_kernel(const ST* __r
 // Many tokens: 16 TF tokens x 64 NF experts per block of four wavefronts (16 NF experts each), through a ring of LDS stages of one 128-byte line of every
 // row, copied by eight consecutive lanes each, the tokens' rows first.  What follows needs rows of whole 16-byte pieces; a last line that is not whole
 // is copied with its first piece in place of those that do not exist, which are taken as zeros of both operands.
-constexpr int kGateTileWaves = 4, kGateStages = 4;
+constexpr int kGateTileWaves = 4, kGateStages = 6;
 template <int TF, int NF>
 struct GateTile {
     static constexpr int kTokens = 16 * TF, kExperts = 64 * NF, kRows = kTokens + kExperts;
@@ -128,9 +128,8 @@ __global__ __launch_bounds__(kGateTileWaves * 64) void gate_tile_kernel(const ST
             from[i] += in < steps - 1 ? 128 : 0;       // behind the last line it is copied again, which keeps up the count that the waits go by
         }
         ++in;
-        in = in >= steps + kGateStages ? in - kGateStages : in;
+        in = in >= steps + kGateStages ? in - kGateStages : in;      // by whole rings
     };
-    static_assert(kGateStages == 4, "the count goes back by whole rings");
 #pragma unroll 1
     for (int i = 0; i < kGateStages - 1; ++i) copy_next();
     f32x4 acc[NF][TF];
@@ -842,15 +841,24 @@ template <typename ST>
 hipError_t launch_gate(const moe_shape& s, const ST* x, const ST* wg, const float* bias, float* logits, hipStream_t stream) {
     const int tokens = (s.T + 15) / 16;
     const bool pieces = ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(wg)) & 15) == 0 && s.d_model % Piece<ST>::kValues == 0;
-    if (pieces && static_cast<long>(tokens) * ((s.E + 15) / 16) > kGateFewBlocks) {
-        const long columns = s.E <= 64 ? 1 : (s.E + 127) / 128;
+    // Of the first kernel a block per CU (two in 32 bits) at the most, and the second from there on; at the next power of two of tokens, the first and the
+    // second, d_model 2048: bf16, 512 tokens x 256 experts 9.3 and 8.6 us, 1024 tokens 16.4 and 8.9; f32, 512 tokens 16.7 and 25.6, 1024 tokens 31.6 and 25.8.
+    // Up to 16 experts leave three quarters of the second's products unused, which counts in 32 bits: 16384 tokens x 8 experts 28.1 and 42.2 (bf16 17.3 and 12.5).
+    constexpr bool kWide = sizeof(ST) == 4;
+    if (pieces && static_cast<long>(tokens) * ((s.E + 15) / 16) > (kWide ? 512 : 256) && !(kWide && s.E <= 16)) {
+        // As few tokens per block as make one round of the CUs, a block each, or the most: 5003 tokens x 256 experts x 2048 in blocks of 16, 32, 48 and
+        // 64 tokens 26.1, 20.9, 13.9 and 15.4 us.
+        const int columns = s.E <= 64 ? 1 : (s.E + 127) / 128, cus = device_cu_count();
+        const int tf = static_cast<int>(std::min(4l, (static_cast<long>(tokens) * columns + cus - 1) / cus));
         if (s.E <= 64) {
-            if (tokens / 4 * columns >= 512) return launch_gate_tile<ST, 4, 1>(s, x, wg, bias, logits, stream);
-            if (tokens / 2 * columns >= 256) return launch_gate_tile<ST, 2, 1>(s, x, wg, bias, logits, stream);
+            if (tf == 4) return launch_gate_tile<ST, 4, 1>(s, x, wg, bias, logits, stream);
+            if (tf == 3) return launch_gate_tile<ST, 3, 1>(s, x, wg, bias, logits, stream);
+            if (tf == 2) return launch_gate_tile<ST, 2, 1>(s, x, wg, bias, logits, stream);
             return launch_gate_tile<ST, 1, 1>(s, x, wg, bias, logits, stream);
         }
-        if (tokens / 4 * columns >= 512) return launch_gate_tile<ST, 4, 2>(s, x, wg, bias, logits, stream);
-        if (tokens / 2 * columns >= 256) return launch_gate_tile<ST, 2, 2>(s, x, wg, bias, logits, stream);
+        if (tf == 4) return launch_gate_tile<ST, 4, 2>(s, x, wg, bias, logits, stream);
+        if (tf == 3) return launch_gate_tile<ST, 3, 2>(s, x, wg, bias, logits, stream);
+        if (tf == 2) return launch_gate_tile<ST, 2, 2>(s, x, wg, bias, logits, stream);
         return launch_gate_tile<ST, 1, 2>(s, x, wg, bias, logits, stream);
     }
     constexpr int kMost = 65535;               // blocks of the grid's second direction
@@ -867,7 +875,9 @@ hipError_t configure_gate() {
     hipError_t e;
     if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 4, 1>), GateTile<4, 1>::kLdsBytes)) != hipSuccess) return e;
     if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 4, 2>), GateTile<4, 2>::kLdsBytes)) != hipSuccess) return e;
+    if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 3, 1>), GateTile<3, 1>::kLdsBytes)) != hipSuccess) return e;
     if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 2, 1>), GateTile<2, 1>::kLdsBytes)) != hipSuccess) return e;
+    if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 3, 2>), GateTile<3, 2>::kLdsBytes)) != hipSuccess) return e;
     if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 2, 2>), GateTile<2, 2>::kLdsBytes)) != hipSuccess) return e;
     if ((e = allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 1, 1>), GateTile<1, 1>::kLdsBytes)) != hipSuccess) return e;
     return allow(reinterpret_cast<const void*>(gate_tile_kernel<ST, 1, 2>), GateTile<1, 2>::kLdsBytes);
@@ -880,12 +890,10 @@ hipError_t launch_gate_logits(const moe_shape& s, const void* x, const void* w_g
     return launch_gate(s, static_cast<const float*>(x), static_cast<const float*>(w_gate), bias, logits, stream);
 }
 
-// Tokens up to which one block does all.
-constexpr int kOneBlockTokens = 128;
-#ifndef KRB
-#define KRB 256
-#endif
-constexpr long kRouteBlocks = KRB;
+// Tokens up to which one block does all, instead of several and a second launch that adds up their counts: 32 tokens x 256 experts 9.6 and 11.8 us
+// (x 8 experts 3.7 and 5.9), 64 tokens 16.9 and 11.8 (5.3 and 6.1).
+constexpr int kOneBlockTokens = 32;
+constexpr long kRouteBlocks = 256;         // 512, which two to a CU would do: 24.0 for 25.1 us of 16384 tokens x 256 experts, and 0.4 us more for the counts
 
 template <int V, bool SIGMOID, bool BALANCED>
 static hipError_t launch_scores(const ScoreArgs& a, hipStream_t stream) {
