@@ -782,18 +782,27 @@ __global__ __launch_bounds__(kTileWaves * 64) void int_product_kernel(const Quan
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------
-// Experts with at least this many rows run in tiles, the others are streamed.
+// Experts with at least this many rows run in tiles, the others are streamed, which are the rows that a streamed unit holds: from 33 rows on in tiles, us,
+// 64 x 2048 x 8192 (rows x N x K) 22.4 for 13.8, 64 x 8192 x 8192 32.5 for 21.9, 33 x 2048 x 2048 10.3 for 9.0.
 constexpr int kTiledMinRows = 65;
 
-// Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave most CUs without one.
+// Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave CUs without one.  A unit takes
+// about 0.25 us per block of its contraction; the second launch 2.5 us and what the parts' sums take on their way to memory and back, 8 bytes of each.  Never
+// cut and cut so, us: 1 x 1024 x 4096 (rows x N x K) 10.4 and 8.1, 16 x 2048 x 8192 17.0 and 9.7, 64 x 2048 x 4096 14.6 and 11.1; not cut, and cut
+// to 256 units: 64 x 8192 x 2048 10.0 and 13.5, 16 x 8192 x 2048 7.5 and 9.0.
 int stream_split(int rows, int N, int K, int E) {
     if (rows == 0 || rows >= kTiledMinRows) return 1;
-    const int units = std::min(rows, E) * quant_blocks(N);
-    return units <= 96 ? std::max(1, std::min(256 / units, quant_blocks(K) / 2)) : 1;
+    const int KB = quant_blocks(K), most = std::min(256 / std::min(256, std::min(rows, E) * quant_blocks(N)), KB / 2);
+    auto us = [&](int parts) { return static_cast<float>((KB + parts - 1) / parts) * 0.25f + (parts > 1 ? 2.5f + static_cast<float>(parts) * rows * N * 2e-6f : 0.f); };
+    int best = 1;
+    for (int parts = 2; parts <= most; ++parts)
+        if (us(parts) < us(best)) best = parts;
+    return best;
 }
 
 // Row fragments per wavefront of the tiled kernel, so rows per tile / 64: large tiles do more per byte, small ones occupy more CUs.
-// Tiles of 256 rows address the rows by 32-bit offsets.
+// Tiles of 256 rows address the rows by 32-bit offsets.  The costs are of a step of a tile, relative; of tiles of 64, 128 and 256 rows, us: 1501 x 1024 x 4096
+// (rows x N x K) 17.1, 22.5 and 32.0, 1024 x 4096 x 4096 29.6, 24.1 and 36.2, 2048 x 4096 x 4096 54.4, 42.4 and 37.4, 8192 x 2048 x 2048 61.3, 47.8 and 42.1.
 int tile_fragments(int rows, int N, size_t operand_bytes) {
     auto cost = [&](int r, float step) {
         const long long units = static_cast<long long>((rows + 64 * r - 1) / (64 * r)) * quant_blocks(N);
