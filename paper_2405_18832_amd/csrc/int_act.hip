@@ -32,6 +32,8 @@ __device__ __forceinline__ bool vanishing(float g) {
     return ACT == MOE_ACT_GELU ? g < -12.f : ACT == MOE_ACT_SILU ? g < -80.f : false;
 }
 
+// One pass, the row in registers from the largest value to the codes.  Bound by memory: gated SiLU of 20011 x 2048 in bf16 43.8 us, 4.7 TB/s read + written (a copy
+// reaches 5.1); 64 x 8192 6.7 us, of which a launch is 3.5.
 template <typename ST, int ACT, bool GATED, int WPR, int WAVES, int NV>
 __global__ __launch_bounds__(WAVES * 64) void act_int_kernel(const IntRowArgs a) {
     static_assert(WPR == 1 || WPR == WAVES, "the block's barriers are the row's");

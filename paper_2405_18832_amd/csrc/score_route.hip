@@ -49,7 +49,8 @@ __device__ __forceinline__ typename Piece<ST>::type load_piece(const ST* row, in
     return __builtin_bit_cast(typename Piece<ST>::type, v);
 }
 
-// 16 tokens x 16 experts per block; its wavefronts take shares of the contraction, which are added up in their order.
+// 16 tokens x 16 experts per block; its wavefronts take shares of the contraction, which are added up in their order.  Bound by a launch and one wait for
+// memory: 32 x 256 x 2048 in bf16 takes 5.5 us, a launch that does nothing 3.5.
 constexpr int kGateWaves = 16;
 template <typename ST>
 __global__ __launch_bounds__(kGateWaves * 64) void gate_few_kernel(const ST* __restrict__ x, const ST* __restrict__ wg, const float* __restrict__ bias,
@@ -88,7 +89,8 @@ __global__ __launch_bounds__(kGateWaves * 64) void gate_few_kernel(const ST* __r
 
 // Many tokens: 16 TF tokens x 64 NF experts per block of four wavefronts (16 NF experts each), through a ring of LDS stages of one 128-byte line of every
 // row, copied by eight consecutive lanes each, the tokens' rows first.  What follows needs rows of whole 16-byte pieces; a last line that is not whole
-// is copied with its first piece in place of those that do not exist, which are taken as zeros of both operands.
+// is copied with its first piece in place of those that do not exist, which are taken as zeros of both operands.  What bounds it is how much is on its way
+// from memory: 5003 x 256 x 2048 in bf16 12.8 us with six stages and a block per CU, 16.4 with four and two blocks; 16384 tokens 30 us, 2.5 TB/s of x.
 constexpr int kGateTileWaves = 4, kGateStages = 6;
 template <int TF, int NF>
 struct GateTile {
@@ -755,7 +757,8 @@ __device__ __forceinline__ void finish_counts(const ScoreArgs& a, int mine, int3
 }
 
 // A block takes `tokens` tokens, 4 per wavefront at a time.  ONE: it is the only block and goes on to the outputs of the
-// counts; else its counts go to the workspace, [block][E] of 16 bits.
+// counts; else its counts go to the workspace, [block][E] of 16 bits.  Bound by vector instructions (1172 per four tokens of 256 experts, which sort a lane's
+// 16 choices and merge eight out of 16 lanes): 16384 tokens take 20 us of the 24 with the counts, all of it in 64 bits 241; one token 6.7 us.
 template <int V>
 constexpr int kRouteScoreWaves = V <= 16 ? 8 : 4;
 template <int V, bool SIGMOID, bool BALANCED, bool ONE>
