@@ -84,7 +84,8 @@ def route(logits, k, score="softmax", balance=None, groups=1, kept=1, top=1, ren
         c = np.where(np.isnan(c), -np.inf, c)
         if groups > 1:
             v = np.where(there & ~np.isnan(p), p, -np.inf) if top == 2 and balance is None else c
-            value = np.sort(v.reshape(groups, size), axis=1)[:, ::-1][:, :top].sum(axis=1)
+            with np.errstate(invalid="ignore"):              # infinity and -infinity
+                value = np.sort(v.reshape(groups, size), axis=1)[:, ::-1][:, :top].sum(axis=1)
             stay = np.argsort(-value, kind="stable")[:kept]
             c = np.where(np.isin(np.arange(E) // size, stay), c, -np.inf)
         order = np.argsort(-c, kind="stable")[:k]

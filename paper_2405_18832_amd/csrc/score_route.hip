@@ -252,7 +252,7 @@ __device__ __forceinline__ uint64_t groups_that_stay(const ScoreArgs& a, const d
             second = fmax(second, fmin(first, c));
             first = fmax(first, c);
         }
-        mine = a.top == 2 ? first + second : first;
+        mine = a.top == 2 ? fmax(first + second, kNone) : first;        // infinity and -infinity: no sum, which is last
         group[lane] = mine;
     }
     __builtin_amdgcn_wave_barrier();

@@ -136,6 +136,14 @@ SIZES = [1, 17, 33, 49, 64, 16, 32, 48, 0, 2, 15, 31, 47, 63, 34, 50]
 
 
 @pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,K", [(1, 100, 1700), (3, 130, 14000), (16, 2000, 9000), (40, 300, 20011), (64, 2048, 4096), (64, 8192, 2048), (64, 4100, 16400), (5, 1, 131071),
+                                   (64, 16, 131071)])
+def test_linear_of_few_rows(gpu_lib, T, N, K, out):
+    """Contractions that are cut into many parts, into a few and not at all, of unequal lengths."""
+    test_linear_large(gpu_lib, T, N, K, out)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("sizes,k,N,K", [
     ([3, 0, 1, 0], 2, 200, 300), ([0, 0, 0, 64], 1, 1024, 2048), ([0, 65], 1, 130, 256), ([64, 65, 0, 129, 1, 257, 130, 0], 2, 384, 200),

@@ -53,6 +53,13 @@ def test_logits(gpu_lib, T, d, E, dtype, offset):
         assert (np.abs(out[:T].double().cpu().numpy() - want) <= (d + 2) * 2.0 ** -23 * size).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,E", [(1300, 96, 64), (2101, 64, 50), (4500, 160, 40), (9000, 64, 33), (13001, 96, 64), (700, 416, 256), (3001, 224, 200), (9001, 96, 65), (13007, 64, 72),
+                                   (70000, 32, 7), (66000, 32, 16)])
+def test_logits_of_blocks_of_every_size(gpu_lib, T, d, E, dtype):
+    test_logits(gpu_lib, T, d, E, dtype, 0)
+
+
 @pytest.mark.parametrize("d", [1, 3, 30, 33, 130, 1001])
 def test_logits_of_odd_widths(gpu_lib, d):
     test_logits(gpu_lib, 50, d, 20, "f32", 1)
@@ -163,6 +170,26 @@ def test_experts_that_are_not_there(gpu_lib, T, E, groups, kept, top, balanced, 
     balance = (0.1 * rng.normal(size=E)).astype(np.float32) if balanced else None
     for renormalize in (False, True):
         check_route(gpu_lib, logits, 8, score=score, balance=balance, groups=groups, kept=kept, top=top, renormalize=renormalize, H=4)
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("T,E,groups,kept,top", [(20, 16, 1, 1, 1), (33, 64, 8, 3, 2), (40, 128, 4, 2, 2), (300, 256, 8, 4, 2), (40, 512, 8, 5, 1)])
+def test_biases_that_are_no_numbers(gpu_lib, T, E, groups, kept, top, score):
+    """A bias of -infinity or NaN takes its expert out, one of infinity takes it first, a large one leaves nothing of the scores' order.  A group of infinity
+    and nothing else has no sum of two and comes last."""
+    rng = np.random.default_rng(E + T)
+    logits = rng.normal(size=(T, E)).astype(np.float32)
+    logits[0, E - 1], logits[1, 3] = -np.inf, np.nan
+    plain = (0.1 * rng.normal(size=E)).astype(np.float32)
+    out, first, large, alone = (plain.copy() for _ in range(4))
+    out[::5], out[1::7] = -np.inf, np.nan
+    first[E // 2 + 1], first[3] = np.inf, np.inf
+    large[:E // 2] = 1e30
+    alone[:E // groups] = -np.inf
+    alone[1] = np.inf
+    for name, balance in [("out", out), ("first", first), ("large", large), ("alone", alone), ("all out", np.full(E, -np.inf, dtype=np.float32))]:
+        say(f"[case] route with a bias {name}: {T} tokens {E} experts {groups} groups {score}")
+        check_route(gpu_lib, logits, 6, score=score, balance=balance, groups=groups, kept=kept, top=top, renormalize=True, H=3)
 
 
 def test_no_tokens(gpu_lib):
