@@ -170,7 +170,7 @@ _SCORE_NAMES = {"softmax": MOE_SCORE_SOFTMAX, "sigmoid": MOE_SCORE_SIGMOID}
 
 
 def make_quant_shape(rows, N, K, E=1, k=1, activation="none", out_dtype="bf16", sums="f32") -> moe_quant_shape:
-    """`activation`: "none" | "relu" | "gelu", `out_dtype`: "f32" | "bf16" | "e4m3" (or the C values).  `sums`: "f32", or "units" for sums by
+    """`activation`: "none" | "relu" | "gelu" | "silu" (int8 products), `out_dtype`: "f32" | "bf16" | "e4m3" (or the C values).  `sums`: "f32", or "units" for sums by
     the matrix units for 8-bit operands (MOE_QUANT_UNIT_SUMS: faster for many rows, less exact; bf16 and e4m3 outputs)."""
     out = int(_DTYPE_NAMES.get(out_dtype, out_dtype)) | {"f32": 0, "units": MOE_QUANT_UNIT_SUMS}[sums]
     return moe_quant_shape(int(rows), int(N), int(K), int(E), int(k), int(_ACT_NAMES.get(activation, activation)), out)
