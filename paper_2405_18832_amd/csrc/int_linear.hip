@@ -55,31 +55,31 @@ __device__ __forceinline__ void finish(int act, const float (&sx)[TF], const uns
 }
 
 // ---- few rows per matrix: the weights are streamed -------------------------------------------------------------------
-// Unit: an expert's rows, at most 64, x 128 NF columns, by 8 wavefronts of 16 NF columns each, a block of 128 columns of the contraction
-// per step.  Bound by memory: what matters is that copies never stop.  Weights and rows go to LDS directly, through a ring of stages that
+// Unit: an expert's rows, at most 64, x 16 NF columns for each of W wavefronts, a block of 128 columns of the contraction per step: 8 wavefronts, or 4
+// where units of 128 columns leave half of the CUs without one.  Bound by memory: what matters is that copies never stop.  Weights and rows go to LDS directly, through a ring of stages that
 // runs on across units; a unit's scales and bias go before its first stage to a place of their own: one more than there are stages, for units of one step.
-// Two experts of 8192 x 2048, a row each, 9.0 us (34 MB), of which a launch is 3.5.
+// Two experts of 8192 x 2048, a row each, 8.3 us (34 MB), of which a launch is 3.5.
 constexpr int kStreamRows = 64, kStreamWaves = 8;
-template <int NF>
+template <int NF, int W>
 struct Streams {
-    static constexpr int kStages = NF == 1 ? 6 : 3, kCols = NF * kQuantBlock;
+    static constexpr int kStages = NF * W == 4 ? 8 : NF == 1 ? 6 : 3, kCols = NF * W * 16, kRowCopies = 8 / W;
     static constexpr int kX = kCols * kQuantBlock, kStage = kX + kStreamRows * kQuantBlock;
     static constexpr int kUnits = kStages * kStage, kPlaces = kStages + 1, kSw = 256, kBias = kSw + kCols * 4, kUnit = kBias + kCols * 4;       // of a unit: scales of rows, columns, bias
-    static constexpr int kList = kUnits + kPlaces * kUnit, kLdsBytes = kList + MOE_MAX_E * 2 + kStreamWaves * 4;
-    static constexpr int kCopies = 2 * NF + 1;          // a wavefront's, per stage
+    static constexpr int kList = kUnits + kPlaces * kUnit, kLdsBytes = kList + MOE_MAX_E * 2 + W * 4;
+    static constexpr int kCopies = 2 * NF + kRowCopies;          // a wavefront's, per stage
     static_assert(kLdsBytes <= 160 * 1024, "fits a CU");
 };
 
 // OUT = kOutParts: the contraction is cut into `split` parts, whose sums go to a.out as [split][rows][pitch of N] int32.
 constexpr int kOutParts = 3;
 
-template <int OUT, int NF, bool SMOOTH>
+template <int OUT, int NF, bool SMOOTH, int W = kStreamWaves>
 __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t* list, int tiles, int parts_wanted, int b, int G, unsigned char* smem) {
-    using S = Streams<NF>;
+    using S = Streams<NF, W>;
     constexpr int kStages = S::kStages, kStage = S::kStage;
     const int split = OUT == kOutParts ? parts_wanted : 1;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15;
-    const int KB = quant_blocks(a.K), blocks = quant_blocks(a.N), groups = (blocks + NF - 1) / NF;
+    const int KB = quant_blocks(a.K), blocks = quant_blocks(a.N), groups = (blocks * 8 + NF * W - 1) / (NF * W);
     const size_t pitch = static_cast<size_t>(KB) * kQuantBlock;
     const int per_tile = groups * split, units = tiles * per_tile;
 
@@ -119,28 +119,33 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
         return w;
     };
 
-    // copies: wavefront w brings rows 8 w ... 8 w + 7, weight fragments NF w ..., and of a unit 64 of its columns' scales or biases and
+    // copies: wavefront w brings rows 8 w ... 8 w + 7 (and 8 (w + W) ...), weight fragments NF w ..., and of a unit 64 of its columns' scales or biases and
     // (all the same) the rows' scales
     const uint32_t lds = lds_address(smem);
     const uint32_t to_weights = lds + wave * NF * kFragBytes, to_rows = lds + S::kX + wave * 1024;
-    const int piece = wave % (4 * NF);
-    const uint8_t *tile_row, *row_from, *weights_from;
+    constexpr int kPieces = S::kCols / 64;
+    const int piece = wave % (2 * kPieces);
+    const uint8_t *tile_row[S::kRowCopies], *weights_from;
+    size_t in_row = 0;
     const float* tile_scale;
     int unit_in = 0;                        // place of the next unit's scales
     auto point_at_tile = [&](const Unit& w) __attribute__((always_inline)) {
-        const int in_tile = wave * 8 + (lane >> 3);
-        tile_row = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(lane, in_tile);
+#pragma unroll
+        for (int i = 0; i < S::kRowCopies; ++i) {
+            const int in_tile = (wave + i * W) * 8 + (lane >> 3);
+            tile_row[i] = a.a + source_row(a, w.row0 + min(in_tile, w.rows - 1)) * pitch + piece_of_lane(lane, in_tile);
+        }
         tile_scale = a.a_scales + source_row(a, w.row0 + min(lane, w.rows - 1));
     };
     auto point_at = [&](const Unit& w) __attribute__((always_inline)) {
-        row_from = tile_row + static_cast<size_t>(w.kb) * kQuantBlock;
+        in_row = static_cast<size_t>(w.kb) * kQuantBlock;
         // columns of the last unit that do not exist are read as the last ones that do, and not stored
-        const int fragment = min(w.group * 8 * NF + wave * NF, blocks * 8 - NF);
+        const int fragment = min((w.group * W + wave) * NF, blocks * 8 - NF);
         weights_from = a.w + static_cast<size_t>(w.e) * quant_matrix_bytes(a.N, a.K) + (static_cast<size_t>(fragment) * KB + w.kb) * kFragBytes + lane * 16;
         if constexpr (OUT != kOutParts) {
-            const float* from = piece < 2 * NF || a.bias == nullptr ? a.w_scales : a.bias;
+            const float* from = piece < kPieces || a.bias == nullptr ? a.w_scales : a.bias;
             const uint32_t to = lds + S::kUnits + unit_in * S::kUnit;
-            copy4_to_lds(from + static_cast<size_t>(w.e) * a.N + min(w.group * S::kCols + (piece % (2 * NF)) * 64 + lane, a.N - 1), to + S::kSw + piece * 256);
+            copy4_to_lds(from + static_cast<size_t>(w.e) * a.N + min(w.group * S::kCols + (piece % kPieces) * 64 + lane, a.N - 1), to + S::kSw + piece * 256);
             copy4_to_lds(tile_scale, to);
             unit_in = unit_in == S::kPlaces - 1 ? 0 : unit_in + 1;
         }
@@ -157,9 +162,10 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
         };
         if (a.once) weights([](const void* from, uint32_t to) __attribute__((always_inline)) { copy16_once_to_lds(from, to); });
         else weights([](const void* from, uint32_t to) __attribute__((always_inline)) { copy16_to_lds(from, to); });
-        copy16_to_lds(row_from, to_rows + at);
+#pragma unroll
+        for (int i = 0; i < S::kRowCopies; ++i) copy16_to_lds(tile_row[i] + in_row, to_rows + at + i * W * 1024);
         weights_from += kFragBytes;
-        row_from += kQuantBlock;
+        in_row += kQuantBlock;
     };
 
     const int tile0 = first / per_tile;
@@ -175,7 +181,7 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
         } else {
             // nothing left to copy: copies of some row to the slot that has fallen free keep up the count that the waits go by
 #pragma unroll
-            for (int i = 0; i < S::kCopies; ++i) copy16_to_lds(tile_row, to_rows + slot_in * kStage);
+            for (int i = 0; i < S::kCopies; ++i) copy16_to_lds(tile_row[0], to_rows + slot_in * kStage);
         }
         slot_in = slot_in == kStages - 1 ? 0 : slot_in + 1;
         ++ahead.kb;
@@ -255,15 +261,16 @@ __device__ __forceinline__ void stream_units(const QuantArgs& a, const uint16_t*
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");       // no copy may land in LDS that is another block's by then
 }
 
-constexpr int kListAt = Streams<1>::kList > Streams<2>::kList ? Streams<1>::kList : Streams<2>::kList;      // behind both rings
+constexpr int kListAt = std::max({Streams<1, 4>::kList, Streams<1, kStreamWaves>::kList, Streams<2, kStreamWaves>::kList});       // behind every ring
 constexpr int kStreamLds = kListAt + MOE_MAX_E * 2 + kStreamWaves * 4;
+static_assert(kStreamLds <= 160 * 1024, "fits a CU");
 
-template <int OUT, bool SMOOTH>
-__global__ __launch_bounds__(kStreamWaves * 64) void int_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
+template <int OUT, bool SMOOTH, int W>
+__global__ __launch_bounds__(W * 64) void int_stream_kernel(const QuantArgs a, int max_rows, int parts_wanted) {
     extern __shared__ __align__(16) unsigned char smem[];
     uint16_t* list = reinterpret_cast<uint16_t*>(smem + kListAt);
-    const int tiles = list_experts<kStreamWaves * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
-    stream_units<OUT, 1, SMOOTH>(a, list, tiles, parts_wanted, blockIdx.x, gridDim.x, smem);
+    const int tiles = list_experts<W * 64>(a, max_rows, list, reinterpret_cast<int32_t*>(list + MOE_MAX_E));
+    stream_units<OUT, 1, SMOOTH, W>(a, list, tiles, parts_wanted, blockIdx.x, gridDim.x, smem);
 }
 
 // Adds up the parts of a split contraction and finishes the rows.  A block of threads per row and 1024 columns, four per thread.
@@ -303,7 +310,7 @@ __global__ __launch_bounds__(256) void int_join_kernel(const QuantArgs a, const 
 //   weights  8 fragments of 2 KiB as they are packed, 16 rows each
 // and a unit's scales and biases go before its first stage to a place of their own, one more than there are stages.
 // Wavefront (wm, wn) of the 4 x 2 multiplies row fragments wm, wm + 4, ... (R of them) and the columns 64 wn ... 64 wn + 63.
-// Bound by a step's copies and its barrier: 16384 x 8192 x 2048, bf16 out, 280 to 287 us (1920 to 1960 TOP/s, matrix units busy 0.41 at 1.9 GHz), 2048 x 4096 x 4096
+// Bound by a step's copies and its barrier: 16384 x 8192 x 2048, bf16 out, 276 to 287 us (1920 to 1990 TOP/s, matrix units busy 0.41 at 1.9 GHz), 2048 x 4096 x 4096
 // 37 (1840), 1501 x 1024 x 4096 15.2.  The sums of a tile of 256 rows wait in registers until the next tile's steps finish and store them (299 us without).
 constexpr int kTileWaves = 8;
 template <int RMAX>
@@ -789,17 +796,23 @@ __global__ __launch_bounds__(kTileWaves * 64) void int_product_kernel(const Quan
 // 64 x 2048 x 8192 (rows x N x K) 22.4 for 13.8, 64 x 8192 x 8192 32.5 for 21.9, 33 x 2048 x 2048 10.3 for 9.0.
 constexpr int kTiledMinRows = 65;
 
-// Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave CUs without one.  A unit takes
-// about 0.25 us per block of its contraction; the second launch 2.5 us and what the parts' sums take on their way to memory and back, 8 bytes of each.  Never
-// cut and cut so, us: 1 x 1024 x 4096 (rows x N x K) 10.4 and 8.1, 16 x 2048 x 8192 17.0 and 9.7, 64 x 2048 x 4096 14.6 and 11.1; not cut, and cut
-// to 256 units: 64 x 8192 x 2048 10.0 and 13.5, 16 x 8192 x 2048 7.5 and 9.0.
+// Units of 128 columns up to which a call of at most 64 rows takes units of half as many, which are then no more than the CUs.  Of 128 and of 64 columns, us:
+// 1 x 16384 x 2048 (rows x N x K) 8.1 and 6.8, 16 x 8192 x 2048 7.9 and 6.6, 64 x 8192 x 2048 10.3 and 8.8, 64 x 16384 x 2048 10.8 and 9.7.
+constexpr int kNarrowUnits = 128;
+
+// Parts that the contraction of a streamed product is cut into: calls of at most 64 rows whose units would leave half of the CUs without one.  A unit takes
+// about 0.2 us per block of its contraction, more with its rows, a part's, of twice the columns, 0.25; the second launch 3.5 us and what the parts' sums take on their
+// way to memory and back, 8 bytes of each.  Never cut and cut so, us: 1 x 1024 x 4096 8.8 and 8.1, 1 x 1024 x 14336 21.8 and 9.9, 16 x 2048 x 8192 14.0 and 9.9,
+// 64 x 2048 x 4096 12.7 and 11.2; not cut, and in four parts: 16 x 8192 x 2048 6.4 and 9.0, 64 x 8192 x 2048 8.7 and 13.5.
 int stream_split(int rows, int N, int K, int E) {
     if (rows == 0 || rows >= kTiledMinRows) return 1;
     const int KB = quant_blocks(K), most = std::min(256 / std::min(256, std::min(rows, E) * quant_blocks(N)), KB / 2);
-    auto us = [&](int parts) { return static_cast<float>((KB + parts - 1) / parts) * 0.25f + (parts > 1 ? 2.5f + static_cast<float>(parts) * rows * N * 2e-6f : 0.f); };
     int best = 1;
-    for (int parts = 2; parts <= most; ++parts)
-        if (us(parts) < us(best)) best = parts;
+    float least = KB * (0.2f + 0.002f * rows);
+    for (int parts = 2; parts <= most; ++parts) {
+        const float us = (KB + parts - 1) / parts * 0.25f + 3.5f + static_cast<float>(parts) * rows * N * 2e-6f;
+        if (us < least) best = parts, least = us;
+    }
     return best;
 }
 
@@ -832,10 +845,11 @@ hipError_t launch_out(const QuantArgs& a, void* ws, hipStream_t stream) {
     if (split > 1) {
         QuantArgs parts = a;
         parts.out = ws;
-        int_stream_kernel<kOutParts, false><<<grid, threads, kStreamLds, stream>>>(parts, a.rows, split);
+        int_stream_kernel<kOutParts, false, kStreamWaves><<<grid, threads, kStreamLds, stream>>>(parts, a.rows, split);
         int_join_kernel<OUT, SMOOTH><<<dim3(a.rows, (a.N + 1023) / 1024), dim3(256), 0, stream>>>(a, static_cast<const int32_t*>(ws), split);
     } else if (a.rows < kTiledMinRows) {
-        int_stream_kernel<OUT, SMOOTH><<<grid, threads, kStreamLds, stream>>>(a, a.rows, 1);
+        if (std::min(a.rows, a.E) * quant_blocks(a.N) <= kNarrowUnits) int_stream_kernel<OUT, SMOOTH, 4><<<grid, dim3(256), kStreamLds, stream>>>(a, a.rows, 1);
+        else int_stream_kernel<OUT, SMOOTH, kStreamWaves><<<grid, threads, kStreamLds, stream>>>(a, a.rows, 1);
     } else {
         const size_t out_bytes = static_cast<size_t>(a.rows) * a.N * elem_size(a.out_dtype);
         const int r = tile_fragments(a.rows, a.N, a.rows / a.k * quant_pitch(a.K));
@@ -857,7 +871,8 @@ hipError_t configure_out() {
     if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 4, SMOOTH, false>), kProductLds<4>)) != hipSuccess) return e;
     if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 2, SMOOTH, false>), kProductLds<2>)) != hipSuccess) return e;
     if ((e = allow_lds(reinterpret_cast<const void*>(int_product_kernel<OUT, 1, SMOOTH, false>), kProductLds<1>)) != hipSuccess) return e;
-    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<OUT, SMOOTH>), kStreamLds);
+    if ((e = allow_lds(reinterpret_cast<const void*>(int_stream_kernel<OUT, SMOOTH, 4>), kStreamLds)) != hipSuccess) return e;
+    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<OUT, SMOOTH, kStreamWaves>), kStreamLds);
 }
 
 // Weights that do not fit the L2s (8 x 4 MiB) are gone before the next call reads them, or have pushed out the rows: streamed units then read
@@ -878,7 +893,7 @@ hipError_t configure_int_kernels() {
     if ((e = configure_out<kOutF32, true>()) != hipSuccess) return e;
     if ((e = configure_out<kOutBf16, false>()) != hipSuccess) return e;
     if ((e = configure_out<kOutBf16, true>()) != hipSuccess) return e;
-    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<kOutParts, false>), kStreamLds);
+    return allow_lds(reinterpret_cast<const void*>(int_stream_kernel<kOutParts, false, kStreamWaves>), kStreamLds);
 }
 
 hipError_t launch_int_product(const QuantArgs& args, void* ws, hipStream_t stream) {
