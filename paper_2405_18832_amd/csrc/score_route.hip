@@ -684,11 +684,18 @@ __device__ __forceinline__ bool choose(const ScoreArgs& a, unsigned char* lds, i
         taken += won ? 1 : 0;
         const float value = BALANCED ? static_cast<float>(best / V) * kUnit : unordered(best);
         if (BALANCED) {
-            const bool apart = before - value > doubt<SIGMOID>(value) + 3.f * kUnit && value > 1.f - kFar;
-            if (!kSettled) unsure |= !apart;
-            else if (j < a.k) in_order &= apart;
-            else if (j == a.k) best_k = apart;
-            else best_k1 = apart;
+            const bool apart = before - value > doubt<SIGMOID>(value) + 3.f * kUnit;
+            // At the range's end all are alike, those that may not be chosen among them (experts of other groups, places past E).  What won there may be any of
+            // them, so no winner that counts may be: none of the k, nor the next one where it is a candidate.
+            const bool alike = !(value > 1.f - kFar);
+            if (!kSettled) unsure |= !apart || alike;
+            else if (j < a.k) {
+                in_order &= apart;
+                unsure |= alike;
+            } else if (j == a.k) {
+                best_k = apart;
+                unsure |= alike && !apart;
+            } else best_k1 = apart;
         } else if (!numbered) unsure |= !(before - value > fmaf(fabsf(value), V * 0x1p-23f, V * 0x1p-126f));
         before = value;
         if (sub == j) mine = min(at, E - 1);
