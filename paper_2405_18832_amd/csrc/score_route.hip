@@ -381,8 +381,11 @@ __device__ __forceinline__ void choose_exactly(const ScoreArgs& a, double* row, 
 // instructions per four tokens of 256 experts, k = 8.)
 //
 // Errors, u = 2^-24.  Sigmoid: its exponential is (|l| + 2) u of itself off, which p (1 - p) weighs (at most 0.23 |l|-fold, 0.25), the sum with one and the
-// reciprocal 3 u: 4 u together.  Softmax: x e^-x <= 0.37 of the exponential's own argument, the sum's and the quotient's 8 u: 9 u.  The bias adds u |c|.
-// Two numbers are in doubt up to `doubt`: twice that and a fifth.  Logits themselves are exact.
+// reciprocal 3 u: 4 u together.  Softmax: an exponential at x below the largest logit, whose own is exact, is (3 x + 2) u of itself off.  Their sum is added
+// up in a tree, 4 + log2 V <= 10 additions deep (one after the other 64 of them would be 63 u off, one large one beside small ones); with Y for the sum of all but the
+// largest, of n experts, x averages ln(n / Y) at the most, and scores of which one is the largest are ((10 + 2) (1 + Y) + Y (3 ln(n / Y) + 2)) / (1 + Y)^2 <= 14 u off
+// each other (n = 1023, Y = 0.3); the smaller one's own exponential and product, 3 x e^-x <= 1.1, 2 and 1, make it 18 u.  The bias adds u |c|.
+// Two numbers are in doubt up to `doubt`: that of both, and a fifth.  Logits themselves are exact.
 template <bool SIGMOID>
 __device__ __forceinline__ float doubt(float c) {
     return 0x1p-24f * fmaf(2.4f, fabsf(c), SIGMOID ? 10.f : 22.f);
@@ -503,6 +506,13 @@ __device__ __forceinline__ void largest_eight(int* v) {
 __host__ __device__ constexpr int score_row_bytes(int E) { return 16 * E; }
 __host__ __device__ constexpr int score_wave_bytes(int E) { return 2 * score_row_bytes(E) + MOE_MAX_GROUPS * 8; }
 
+// Pairs, pairs of pairs, ...: log2 V additions deep.
+template <int V>
+__device__ __forceinline__ float tree_sum(const float* v) {
+    if constexpr (V == 1) return v[0];
+    else return tree_sum<V / 2>(v) + tree_sum<V / 2>(v + V / 2);
+}
+
 constexpr int kFastGroups = 16;
 template <int V, bool SIGMOID, bool BALANCED>
 __device__ __forceinline__ bool choose(const ScoreArgs& a, unsigned char* lds, int lane, bool live, long t, long last, int32_t* hist) {
@@ -539,9 +549,10 @@ __device__ __forceinline__ bool choose(const ScoreArgs& a, unsigned char* lds, i
 #pragma unroll
         for (int q = 0; q < V; ++q) most = fmaxf(most, c[q]);
         most = unordered(most_of(ordered(most)));
-        total = 0.f;
+        float e[V];
 #pragma unroll
-        for (int q = 0; q < V; ++q) total += __builtin_amdgcn_exp2f((c[q] - most) * kLog2e);
+        for (int q = 0; q < V; ++q) e[q] = __builtin_amdgcn_exp2f((c[q] - most) * kLog2e);
+        total = tree_sum<V>(e);
         total = row_reduce(total, [](float u, float v) { return u + v; });
     }
     const float by = SIGMOID ? 1.f : 1.f / total;

@@ -44,3 +44,23 @@ def test_finite_biases_that_take_experts_out(gpu_lib, E, k, groups, kept, top, s
             check_route(gpu_lib, rounded(logits[:20], "bf16"), k, dtype="bf16", **rule)         # one block
             idx = run_route(gpu_lib, logits, k, **rule)[0]
             assert all(len(set(row)) == k and len(set(row // (E // groups))) <= kept for row in idx)
+
+
+def test_softmax_of_one_large_score_and_many_small_ones(gpu_lib):
+    """1024 experts: a score of nearly one, 63 of half a step of fp32 or so beside it (which a running sum of 32 bits would lose, one by one), and a bias between what is
+    left of it with and without them."""
+    u = 2.0 ** -24
+    for first, place in [(0, 20), (0, 700), (64 * 15 + 3, 20), (1, 1000)]:
+        logits = np.full((40, 1024), -50.0, dtype=np.float32)
+        lane = [64 * j + 4 * (first % 64 // 4) + i for j in range(16) for i in range(4)]       # the experts of a lane
+        logits[:, lane] = -16.75
+        logits[:, first] = 0
+        for t in range(40):                                     # fewer and fewer of them
+            logits[t, lane[64 - t:]] = np.where(np.asarray(lane[64 - t:]) == first, 0, -50).astype(np.float32)
+        for steps in (8, 24, 40, 52):
+            say(f"[case] softmax of 1024 experts, one large, bias {steps} steps below one at {place}")
+            balance = np.zeros(1024, dtype=np.float32)
+            balance[place] = 1 - steps * u
+            for k in (1, 3):
+                check_route(gpu_lib, logits, k, balance=balance)
+            check_route(gpu_lib, logits, 2, balance=balance, groups=16, kept=8, top=1)
