@@ -390,6 +390,12 @@ template <bool SIGMOID>
 __device__ __forceinline__ float doubt(float c) {
     return 0x1p-24f * fmaf(2.4f, fabsf(c), SIGMOID ? 10.f : 22.f);
 }
+// How far the value of one group may be off: the constant above, which is that of two scores; and one unit each of its choices' magnitudes for the bias, for the sum and for
+// adding this to it.  Not of the sum's own magnitude: choices may cancel.
+template <bool SIGMOID>
+__device__ __forceinline__ float group_doubt(float size) {
+    return 0x1p-24f * fmaf(3.2f, size, SIGMOID ? 10.f : 22.f);
+}
 typedef uint32_t any_u32x2 __attribute__((ext_vector_type(2), aligned(2)));
 __device__ __forceinline__ void load_four(const float* p, float* v) {
     const any_f32x4 w = *reinterpret_cast<const any_f32x4*>(p);
@@ -616,9 +622,10 @@ __device__ __forceinline__ bool choose(const ScoreArgs& a, unsigned char* lds, i
         }
         bool stays = g < a.groups && ahead < a.kept;
         if (BALANCED || by_score) {
-            const float low = unordered(least_of(ordered(stays ? mine : -kLow)));
-            const float high = unordered(most_of(ordered(g < a.groups && !stays ? mine : kLow)));
-            const bool close = !(low - high > 2.f * doubt<SIGMOID>(low));        // sums of two
+            const float size = a.top == 2 ? fabsf(first) + fabsf(second) : fabsf(first), off = group_doubt<SIGMOID>(size);
+            const float low = unordered(least_of(ordered(stays ? mine - off : -kLow)));
+            const float high = unordered(most_of(ordered(g >= a.groups ? kLow : !(size < 0x1p+100f) ? -kLow : !stays ? mine + off : kLow)));
+            const bool close = !(low > high);
             if (SIGMOID) {                     // 64 bits say which groups stay, a token at a time
                 __builtin_amdgcn_wave_barrier();
                 uint64_t left = __ballot(close && live && sub == 0);

@@ -64,3 +64,36 @@ def test_softmax_of_one_large_score_and_many_small_ones(gpu_lib):
             for k in (1, 3):
                 check_route(gpu_lib, logits, k, balance=balance)
             check_route(gpu_lib, logits, 2, balance=balance, groups=16, kept=8, top=1)
+
+
+def test_groups_whose_choices_cancel(gpu_lib):
+    """Two groups of two experts with biases of 7.25 and -8.75: the sums are near zero, the choices' roundings are not.  The scores are such that with fp32 scores to nearest
+    the roundings add up, 12 steps of 2^-24 for each group, the other way round for one than for the other, and the better group's sum is less than a step above."""
+    u, up, down = 2.0 ** -24, 7.25, -8.75
+    l = np.arange(1 << 21, dtype=np.float64) * 2.0 ** -25 + 0.3
+    l = l.astype(np.float32)
+    p = 1 / (1 + np.exp(-l.astype(np.float64))) / u
+    part, n = p % 16, np.floor(p / 16)                          # choices near 8: multiples of 16 steps, near 7: of 8
+    part8, n8 = p % 8, np.floor(p / 8)
+    even, even8 = n % 2 == 0, n8 % 2 == 0
+    a1, a2 = np.flatnonzero(even8 & (part8 > 4.2) & (part8 < 4.45)), np.flatnonzero(even & (part > 8.2) & (part < 8.45))
+    b1, b2 = np.flatnonzero(even8 & (part8 > 4.5) & (part8 < 4.7)), np.flatnonzero(~even & (part > 7.55) & (part < 7.8))
+    at = {int(n8[i]): i for i in b1}
+    rng = np.random.default_rng(1)
+    rows = []
+    while len(rows) < 4096:
+        i, j, h = rng.choice(a1), rng.choice(a2), rng.choice(b2)
+        g = at.get(int(n8[i] + 2 * n[j] - 2 * n[h]))
+        if g is not None and p[i] + p[j] > p[g] + p[h] + 0.1:
+            rows.append([l[i], l[j], l[g], l[h]])
+    logits = np.asarray(rows, dtype=np.float32)
+    logits[1::2] = logits[1::2][:, [2, 3, 0, 1]]
+    balance = np.array([up, down, up, down], dtype=np.float32)
+    for k in (1, 2):
+        say(f"[case] groups whose choices cancel, k {k}")
+        check_route(gpu_lib, logits, k, score="sigmoid", balance=balance, groups=2, kept=1, top=2)
+    wide = np.full((4096, 32), -20.0, dtype=np.float32)         # more groups, others far below
+    wide[:, [8, 9, 24, 25]] = logits
+    balance = np.full(32, -9.0, dtype=np.float32)
+    balance[[8, 9, 24, 25]] = up, down, up, down
+    check_route(gpu_lib, wide, 4, score="sigmoid", balance=balance, groups=4, kept=1, top=2)
