@@ -442,8 +442,8 @@ typedef struct {
  *   topk_w  [T, k]: p of these (shape->renormalize: divided by their sum; zero where that is zero), times scale;
  *   counts [E], offsets [E + 1], H, hot_mask: as moe_route.
  * Scores are compared in 64 bits, so that the choice is the formulas', however close two of them are.
- * A logit of -infinity marks an expert that is not there: it is chosen after all others (so only where fewer than k are left, lowest index
- * first, with weight zero), and so is one whose c is -infinity or NaN; a group whose sum is NaN counts as one of -infinity.  The weights of a
+ * A logit of -infinity marks an expert that is not there: it is chosen after the kept groups' others (so only where fewer than k of
+ * them are left, lowest index first, with weight zero), and so is one whose c is -infinity or NaN; a group whose sum is NaN counts as one of -infinity.  The weights of a
  * token with a NaN among its logits (softmax: or +infinity) are NaN.
  * T, E, k and renormalize of `shape` enter, dtype and widths need only be valid.  ws: at least moe_workspace_bytes(shape).
  */

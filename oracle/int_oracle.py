@@ -87,8 +87,10 @@ def route(logits, k, score="softmax", balance=None, groups=1, kept=1, top=1, ren
             with np.errstate(invalid="ignore"):              # infinity and -infinity
                 value = np.sort(v.reshape(groups, size), axis=1)[:, ::-1][:, :top].sum(axis=1)
             stay = np.argsort(-value, kind="stable")[:kept]
-            c = np.where(np.isin(np.arange(E) // size, stay), c, -np.inf)
-        order = np.argsort(-c, kind="stable")[:k]
+            kept_ones = np.flatnonzero(np.isin(np.arange(E) // size, stay))
+        else:
+            kept_ones = np.arange(E)
+        order = kept_ones[np.argsort(-c[kept_ones], kind="stable")[:k]]
         w = np.where(c[order] > -np.inf, p[order], 0.0)
         if renormalize:
             w = w / w.sum() if w.sum() > 0 else np.zeros(k)

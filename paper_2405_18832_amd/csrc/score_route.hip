@@ -317,7 +317,7 @@ __device__ __forceinline__ void choose_exactly(const ScoreArgs& a, double* row, 
 #pragma unroll 1
         for (int e = lane; e < E; e += 64) {
             const float l = values[e];
-            if (!(stay >> (e / size) & 1)) row[e] = kNone;
+            if (!(stay >> (e / size) & 1)) row[e] = __builtin_nan("");          // taken: not even where the kept groups have no other than masked experts left
             else if (by_score) row[e] = l > kLow ? static_cast<double>(l) : kNone;
         }
         __builtin_amdgcn_wave_barrier();

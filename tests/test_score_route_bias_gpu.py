@@ -97,3 +97,34 @@ def test_groups_whose_choices_cancel(gpu_lib):
     balance = np.full(32, -9.0, dtype=np.float32)
     balance[[8, 9, 24, 25]] = up, down, up, down
     check_route(gpu_lib, wide, 4, score="sigmoid", balance=balance, groups=4, kept=1, top=2)
+
+
+@pytest.mark.parametrize("score", ["sigmoid", "softmax"])
+@pytest.mark.parametrize("balanced", [False, True])
+@pytest.mark.parametrize("E,k,groups,kept,top", [(8, 3, 2, 1, 1), (32, 6, 4, 2, 1), (64, 8, 8, 2, 2), (256, 8, 8, 1, 1), (80, 8, 20, 3, 1), (600, 8, 4, 2, 2)])
+def test_masked_experts_of_the_kept_groups_come_before_other_groups(gpu_lib, E, k, groups, kept, top, balanced, score):
+    """Where fewer than k experts are left in the kept groups, the others are those groups' masked ones, lowest index first: never an expert of a group that was dropped."""
+    say(f"[case] masked experts of kept groups {E} k {k} groups {groups}/{kept} top {top} {score} {balanced}")
+    rng = np.random.default_rng(E + k)
+    size, T = E // groups, 60
+    logits = rng.normal(size=(T, E)).astype(np.float32)
+    best = np.stack([rng.permutation(groups)[:kept] for _ in range(T)])
+    for t in range(T):
+        for g in best[t]:                                       # two large ones each, the rest masked
+            logits[t, g * size:(g + 1) * size] = -np.inf
+            logits[t, g * size + rng.permutation(size)[:2]] = [6, 5]
+    balance = (0.01 * rng.normal(size=E)).astype(np.float32) if balanced else None
+    idx, w, counts, offsets, _ = run_route(gpu_lib, logits, k, score=score, balance=balance, groups=groups, kept=kept, top=top)
+    l = logits.astype(np.float64)
+    p = 1 / (1 + np.exp(-l)) if score == "sigmoid" else np.exp(l) / np.exp(l).sum(axis=1, keepdims=True)
+    short = 0
+    for t in range(T):
+        c = np.where(np.isneginf(l[t]), -np.inf, p[t] + balance if balanced else l[t])
+        of = np.where(np.isneginf(l[t]), -np.inf, p[t]) if top == 2 and not balanced else c
+        value = np.sort(of.reshape(groups, size), axis=1)[:, size - top:].sum(axis=1)
+        stay = set(sorted(range(groups), key=lambda g: (-value[g], g))[:kept])
+        want = sorted((e for e in range(E) if e // size in stay), key=lambda e: (-c[e], e))[:k]
+        assert list(idx[t]) == want and ((w[t] > 0) == (c[want] > -np.inf)).all(), (t, idx[t], want)
+        short += np.isneginf(c[want[-1]])
+    assert short >= T // 2
+    assert np.array_equal(counts, np.bincount(idx.reshape(-1), minlength=E))
