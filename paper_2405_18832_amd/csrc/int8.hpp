@@ -11,8 +11,8 @@ static_assert(128ll * 128 * MOE_INT_MAX_K <= 0x7fffffffll, "sums of products of 
 #ifdef __HIPCC__
 constexpr float kIntMax = 127.f;
 
-// z / (1 + exp(-z)), by the hardware's exponential and reciprocal: the exponent's argument is |z| log2 e 2^-24 off at most, so the result
-// (|z| + 4) 2^-24 of itself.
+// z / (1 + exp(-z)), by the hardware's exponential and reciprocal (a unit of the last place each, so 2 u, u = 2^-24): the constant is 0.22 u off, the argument's product u,
+// so the result (1.25 |z| + 6) u of itself.
 __device__ __forceinline__ float silu(float z) { return z * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(z * -1.4426950408889634f)); }
 
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {

@@ -18,19 +18,18 @@ __device__ __forceinline__ double act_exact(double g, float least) {
     if (ACT == MOE_ACT_SILU) return g / (1.0 + exp(-g));
     return g < static_cast<double>(least) ? static_cast<double>(least) : g;
 }
-// Twice the relative error of act_value * u * ratio (whose divisor has the same) for arguments up to g in magnitude.  GeLU: 8.4e-7 down to -4; below, its
-// argument z^2 / 2 log2 e is |z| times that of SiLU's.
+// Twice the relative error of act_value * u, and of half of the quotient's roundings, for arguments up to g in magnitude.  SiLU, u = 2^-24: (1.25 |g| + 6) u (int8.hpp), the
+// product and the quotient one each.  GeLU: 8.4e-7 down to -4; below, its argument z^2 / 2 log2 e is |z| times that of SiLU's.
 template <int ACT>
 __device__ __forceinline__ float act_slack(float g) {
     if (ACT == MOE_ACT_GELU) return fmaf(g * g, 0x1p-22f, 0x1p-18f);
-    if (ACT == MOE_ACT_SILU) return fmaf(g, 0x1p-22f, 0x1p-20f);
+    if (ACT == MOE_ACT_SILU) return fmaf(g, 0x1.4p-23f, 0x1p-20f);
     return kProductSlack;
 }
-// Where act_value has nothing left of a number that a large second factor could make the row's largest again.
+// Gates below this leave nothing to act_value of a number that a large second factor could make the row's largest again.
 template <int ACT>
-__device__ __forceinline__ bool vanishing(float g) {
-    return ACT == MOE_ACT_GELU ? g < -12.f : ACT == MOE_ACT_SILU ? g < -80.f : false;
-}
+constexpr float kTail = ACT == MOE_ACT_GELU ? -12.f : -80.f;
+constexpr float kHuge = __builtin_huge_valf();
 
 // One pass, the row in registers from the largest value to the codes.  Bound by memory: gated SiLU of 20011 x 2048 in bf16 43.8 us, 4.7 TB/s read + written (a copy
 // reaches 5.1); 64 x 8192 6.7 us, of which a launch is 3.5.
@@ -55,19 +54,36 @@ __global__ __launch_bounds__(WAVES * 64) void act_int_kernel(const IntRowArgs a)
     auto column = [&](int chunk) { return chunk * kChunk + lane * 8; };
     constexpr int kKept = NV > 0 ? NV : 1;
     float v[kKept][8], slack[kKept];
+    // Values that act_value does not hold are left out of a row that has any, which is looked through again then (`apart`); their own slack says so, a negative one, and
+    // before that an infinite one.
+    constexpr bool kApart = GATED && kSmooth;
+    bool apart = kApart && NV == 0;
     auto value = [&](const float (&g)[8], const float (&u)[GATED ? 8 : 1], float (&to)[8], float& own) __attribute__((always_inline)) {
         float size = 0.f;
-        bool vanishes = false;
+        uint32_t lowest = 0;                                // bits: of negative numbers, the larger the lower
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             to[i] = act_value<ACT>(g[i], least);
-            if constexpr (GATED) {
-                to[i] *= u[i];
-                vanishes |= vanishing<ACT>(g[i]);
-            }
+            if constexpr (GATED) to[i] *= u[i];
+            if (kApart) lowest = max(lowest, __float_as_uint(g[i]));
             if (kSmooth) size = fmaxf(size, fabsf(g[i]));
         }
-        own = GATED && vanishes ? -1.f : act_slack<ACT>(size);
+        own = act_slack<ACT>(size);
+        if constexpr (kApart) {
+            const bool any = lowest > __builtin_bit_cast(uint32_t, kTail<ACT>);
+            if (!apart) {
+                own = any ? kHuge : own;
+            } else if (any) {
+                size = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const bool out = g[i] < kTail<ACT>;
+                    to[i] = out ? fmaf(g[i], 0.f, u[i] * 0.f) : to[i];      // zero, or NaN where an infinity or a NaN makes the row none
+                    size = fmaxf(size, out ? 0.f : fabsf(g[i]));
+                }
+                own = -act_slack<ACT>(size);
+            }
+        }
     };
     auto each = [&](auto f) __attribute__((always_inline)) {       // f(chunk, values, slack)
         if constexpr (NV > 0) {
@@ -84,40 +100,48 @@ __global__ __launch_bounds__(WAVES * 64) void act_int_kernel(const IntRowArgs a)
             }
         }
     };
-    uint32_t most = 0;
-    float loosest = 0.f;
-    if (live) {
-        if constexpr (NV > 0) {                             // all loads first
-            float g[NV][8], u[NV][GATED ? 8 : 1];
-            unrolled<NV>([&](auto j) __attribute__((always_inline)) {
-                if (j * WPR + part < chunks) {
-                    load8<ST, false>(g_row, column(j * WPR + part), d, g[j]);
-                    if constexpr (GATED) load8<ST, false>(u_row, column(j * WPR + part), d, u[j]);
-                }
-            });
-            unrolled<NV>([&](auto j) __attribute__((always_inline)) {
-                if (j * WPR + part < chunks) value(g[j], u[j], v[j], slack[j]);
-            });
-        }
-        each([&](int, const float (&values)[8], float own) __attribute__((always_inline)) {
-            loosest = fmaxf(loosest, own < 0.f ? 1.f : own);
+    uint32_t most;
+    float loosest;
+#pragma unroll 1
+    while (true) {
+        most = 0;
+        loosest = 0.f;
+        if (live) {
+            if constexpr (NV > 0) {                             // all loads first
+                float g[NV][8], u[NV][GATED ? 8 : 1];
+                unrolled<NV>([&](auto j) __attribute__((always_inline)) {
+                    if (j * WPR + part < chunks) {
+                        load8<ST, false>(g_row, column(j * WPR + part), d, g[j]);
+                        if constexpr (GATED) load8<ST, false>(u_row, column(j * WPR + part), d, u[j]);
+                    }
+                });
+                unrolled<NV>([&](auto j) __attribute__((always_inline)) {
+                    if (j * WPR + part < chunks) value(g[j], u[j], v[j], slack[j]);
+                });
+            }
+            each([&](int, const float (&values)[8], float own) __attribute__((always_inline)) {
+                loosest = fmaxf(loosest, kApart && own < 0.f ? fmaxf(-own, 0x1p-17f) : own);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) most = max(most, magnitude(values[i]));
-        });
-    }
-    most = wave_max(most);
-    if (kSmooth) loosest = __uint_as_float(wave_max(__float_as_uint(loosest)));
-    if constexpr (WPR > 1) {
-        if (lane == 0) {
-            shared.most[wave] = most;
-            shared.slack[wave] = loosest;
+                for (int i = 0; i < 8; ++i) most = max(most, magnitude(values[i]));
+            });
         }
-        __syncthreads();
+        most = wave_max(most);
+        if (kSmooth) loosest = __uint_as_float(wave_max(__float_as_uint(loosest)));
+        if constexpr (WPR > 1) {
+            if (lane == 0) {
+                shared.most[wave] = most;
+                shared.slack[wave] = loosest;
+            }
+            __syncthreads();
 #pragma unroll
-        for (int w = 0; w < WPR; ++w) {
-            most = max(most, shared.most[w]);
-            loosest = fmaxf(loosest, shared.slack[w]);
+            for (int w = 0; w < WPR; ++w) {
+                most = max(most, shared.most[w]);
+                loosest = fmaxf(loosest, shared.slack[w]);
+            }
         }
+        if (!kApart || apart || __builtin_amdgcn_readfirstlane(__float_as_int(loosest)) < __float_as_int(kHuge)) break;
+        apart = true;
+        if constexpr (WPR > 1) __syncthreads();             // `shared` is written again
     }
     write_row<WPR, WAVES>(shared, live, most >= 0x7f800000u, most, loosest, 1.0, d, a.q + static_cast<size_t>(live ? row : 0) * quant_pitch(d),
                           a.q_scales + (live ? row : 0), each, [&](int chunk, int i) __attribute__((always_inline)) {

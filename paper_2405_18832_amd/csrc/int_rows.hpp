@@ -99,11 +99,12 @@ struct Quotient {
 };
 
 // From a row's fp32 values to its codes and scale; called by all wavefronts of a block, the row's WPR among them.
-//   each(f): f(chunk, values [8], slack) for the wavefront's chunks; slack: relative error of their quotients, negative where nothing is said of them.
-//   exact(chunk, i): the value in 64 bits.   most: bits of the row's largest magnitude.   slack: the row's largest, below 2^-17 where the scale may
-//   come from it.   factor: what the values are multiplied by for the scale.   bad: the row is none.   pitch: bytes of a row of codes.
-// Codes are written from fp32; those in doubt, most often none or a few of a row, are written again, for which the row's largest value in 64 bits is
-// needed first.
+//   each(f): f(chunk, values [8], slack) for the wavefront's chunks; slack: twice the relative error of the values, negative where some of the lane's are left out,
+//   which are zero then (all of these are computed in 64 bits).
+//   exact(chunk, i): the value in 64 bits.   most: bits of the row's largest magnitude.   slack: the row's largest, below 2^-17 where quotients by that magnitude, and
+//   the scale, may be taken from it; 2^-17 at least where values are left out.   factor: what the values are multiplied by for the scale.   bad: the row is none.
+// Codes are written from fp32, a quotient's error being that of its value and that of the largest, half of either slack; those in doubt, most often none or a few of a
+// row, are written again, for which the row's largest value in 64 bits is needed first.  Where fp32's is not exact enough all are, as quotients by that.
 template <int WPR, int WAVES, typename Each, typename Exact>
 __device__ __forceinline__ void write_row(RowShared<WAVES>& shared, bool live, bool bad, uint32_t most, float slack, double factor, int d, uint8_t* q,
                                           float* q_scale, Each each, Exact exact) {
@@ -114,16 +115,17 @@ __device__ __forceinline__ void write_row(RowShared<WAVES>& shared, bool live, b
     // values too large or too small for fp32's quotients, or a scale that might be the smallest one: all of them from 64 bits
     const bool extreme = !(largest >= 0x1p-100f && largest <= 0x1p+100f) || !(largest_out >= 0x1p-110 && largest_out <= 0x1p+110);
     const float ratio = extreme ? 0.f : kIntMax / largest;
+    const bool loose = !(slack < 0x1p-17f);
     bool doubt = false;
     if (live) {
         each([&](int chunk, const float (&v)[8], float own) __attribute__((always_inline)) {
             const int c = chunk * kChunk + lane * 8;
-            const Codes8 codes = codes8(v, ratio, [&](int) { return own; });
+            const Codes8 codes = codes8(v, ratio, [&](int) { return fmaf(0.5f, own, 0.5f * slack); });
             doubt |= codes.unsure != 0 || own < 0.f;
             if (c < pitch) *reinterpret_cast<uint2*>(q + c) = bad || extreme ? uint2{0, 0} : uint2{codes.lo, codes.hi};
         });
     }
-    doubt = live && !bad && (doubt || extreme || !(slack < 0x1p-17f));
+    doubt = live && !bad && (doubt || extreme || loose);
     bool any = __ballot(doubt) != 0;
     if constexpr (WPR > 1) any = __syncthreads_or(any) != 0;
     double top = largest;
@@ -132,10 +134,11 @@ __device__ __forceinline__ void write_row(RowShared<WAVES>& shared, bool live, b
         if (live && !bad) {
             each([&](int chunk, const float (&v)[8], float own) __attribute__((always_inline)) {
                 const int c = chunk * kChunk + lane * 8;
+                const float least = extreme || own < 0.f ? 0.f : largest * (1.f - (own + slack + 0x1p-16f));
                 uint32_t next = 0;                          // values that may be the largest
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    next |= c + i < d && (extreme || own < 0.f || fabsf(v[i]) >= largest * (1.f - fmaf(2.f, own, 0x1p-16f))) ? 1u << i : 0u;
+                for (int i = 0; i < 8; ++i) next |= fabsf(v[i]) >= least ? 1u << i : 0u;
+                next &= c + 8 <= d ? 0xffu : c < d ? 0xffu >> (c + 8 - d) : 0u;
                 while (next != 0) {
                     const int i = __builtin_ctz(next);
                     next &= next - 1;
@@ -154,9 +157,13 @@ __device__ __forceinline__ void write_row(RowShared<WAVES>& shared, bool live, b
         if (live) {
             bad = bad || !(top * factor <= static_cast<double>(FLT_MAX));
             const Quotient quotient{top, factor, top * factor < 127.0 * 0x1p-126};
+            const bool again = loose && !extreme;
+            const float by = again ? kIntMax / static_cast<float>(top) : ratio, divisor = again ? 0x1p-22f : 0.5f * slack;
             each([&](int chunk, const float (&v)[8], float own) __attribute__((always_inline)) {
                 const int c = chunk * kChunk + lane * 8;
-                uint32_t unsure = extreme || own < 0.f || bad ? 0xffu : codes8(v, ratio, [&](int) { return own; }).unsure;
+                const Codes8 codes = codes8(v, by, [&](int) { return fmaf(0.5f, own, divisor); });
+                if (again && c < pitch) *reinterpret_cast<uint2*>(q + c) = bad ? uint2{0, 0} : uint2{codes.lo, codes.hi};
+                uint32_t unsure = extreme || own < 0.f || bad ? 0xffu : codes.unsure;
                 while (unsure != 0) {
                     const int i = __builtin_ctz(unsure);
                     unsure &= unsure - 1;
