@@ -29,6 +29,9 @@ __device__ __forceinline__ float act_slack(float g) {
 // Gates below this leave nothing to act_value of a number that a large second factor could make the row's largest again.
 template <int ACT>
 constexpr float kTail = ACT == MOE_ACT_GELU ? -12.f : -80.f;
+// And gates of which half is below fp32's normal numbers lose some of it there.  They take factors of 2^20 and more to be seen in a row whose largest value is 2^-100 and more
+// (below, all of it is computed in 64 bits).
+constexpr float kSmallGate = 0x1p-124f, kLargeFactor = 0x1p+20f;
 constexpr float kHuge = __builtin_huge_valf();
 
 // One pass, the row in registers from the largest value to the codes.  Bound by memory: gated SiLU of 20011 x 2048 in bf16 43.8 us, 4.7 TB/s read + written (a copy
@@ -59,29 +62,34 @@ __global__ __launch_bounds__(WAVES * 64) void act_int_kernel(const IntRowArgs a)
     constexpr bool kApart = GATED && kSmooth;
     bool apart = kApart && NV == 0;
     auto value = [&](const float (&g)[8], const float (&u)[GATED ? 8 : 1], float (&to)[8], float& own) __attribute__((always_inline)) {
-        float size = 0.f;
+        float size = 0.f, widest = 0.f;
         uint32_t lowest = 0;                                // bits: of negative numbers, the larger the lower
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             to[i] = act_value<ACT>(g[i], least);
             if constexpr (GATED) to[i] *= u[i];
-            if (kApart) lowest = max(lowest, __float_as_uint(g[i]));
+            if constexpr (kApart) {
+                lowest = max(lowest, __float_as_uint(g[i]));
+                widest = fmaxf(widest, fabsf(u[i]));
+            }
             if (kSmooth) size = fmaxf(size, fabsf(g[i]));
         }
         own = act_slack<ACT>(size);
         if constexpr (kApart) {
-            const bool any = lowest > __builtin_bit_cast(uint32_t, kTail<ACT>);
+            const bool any = lowest > __builtin_bit_cast(uint32_t, kTail<ACT>) || widest >= kLargeFactor;
             if (!apart) {
                 own = any ? kHuge : own;
             } else if (any) {
                 size = 0.f;
+                bool left = false;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const bool out = g[i] < kTail<ACT>;
+                    const bool out = g[i] < kTail<ACT> || (fabsf(g[i]) < kSmallGate && g[i] != 0.f);
+                    left |= out;
                     to[i] = out ? fmaf(g[i], 0.f, u[i] * 0.f) : to[i];      // zero, or NaN where an infinity or a NaN makes the row none
                     size = fmaxf(size, out ? 0.f : fabsf(g[i]));
                 }
-                own = -act_slack<ACT>(size);
+                own = left ? -act_slack<ACT>(size) : act_slack<ACT>(size);
             }
         }
     };

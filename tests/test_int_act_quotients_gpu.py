@@ -47,3 +47,23 @@ def test_rows_of_which_only_the_tail_is_left(gpu_lib):
         h[:, 77], h[:, 677] = z, 2e38
         h[9, 677], h[10, 677], h[11, 77] = np.inf, np.nan, -np.inf
         act_case(gpu_lib, rounded(h, "f32"), act, 1, "f32")
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "silu"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("f", [40, 700, 9000])
+def test_gates_below_the_normal_numbers(gpu_lib, act, dtype, f):
+    """The other factor brings back what the gate's rounding there would have lost."""
+    say(f"[case] act gates below the normal numbers {act} {dtype} {f}")
+    rng = np.random.default_rng(f)
+    step = 2.0 ** (-149 if dtype == "f32" else -133)
+    h = np.zeros((40, 2 * f))
+    g, u = h[:, :f], h[:, f:]
+    for r in range(40):
+        places = [0, f - 1] if r % 4 == 0 else rng.permutation(f)[:1 + r] if r % 4 == 1 else np.arange(f)
+        g[r], u[r] = 1e-7 * rng.normal(size=f), rng.normal(size=f)
+        g[r, places] = rng.integers(1, 9 if r < 20 else 100, len(places)) * step * rng.choice([-1, 1], len(places))
+        u[r, places] = 2.0 ** (125 if dtype == "f32" else 109) * rng.uniform(0.5, 2, len(places))
+        if r % 4 == 3:
+            u[r, ::2] *= 2.0 ** -30                             # what is left there is below the others' half steps
+    act_case(gpu_lib, rounded(h, dtype), act, 1, dtype)
