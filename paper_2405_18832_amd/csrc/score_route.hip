@@ -859,10 +859,15 @@ namespace {
 template <typename ST, int TF, int NF>
 hipError_t launch_gate_tile(const moe_shape& s, const ST* x, const ST* wg, const float* bias, float* logits, hipStream_t stream) {
     using G = GateTile<TF, NF>;
+    constexpr long kMost = 0xffffffffl / (kGateTileWaves * 64) / 8 * 8;        // blocks of a launch, which counts at most 2^32 - 1 threads
     const int groups = (s.E + G::kExperts - 1) / G::kExperts;
-    const long blocks = (s.T + G::kTokens - 1l) / G::kTokens * groups;
-    gate_tile_kernel<ST, TF, NF><<<dim3(static_cast<unsigned>((blocks + 7) / 8 * 8)), dim3(kGateTileWaves * 64), G::kLdsBytes, stream>>>(
-        x, wg, bias, logits, s.T, s.d_model, s.E, groups);
+    const long most = kMost / groups * G::kTokens;
+    for (long t0 = 0; t0 < s.T; t0 += most) {
+        const int tokens = static_cast<int>(std::min(s.T - t0, most));
+        const long blocks = (tokens + G::kTokens - 1l) / G::kTokens * groups;
+        gate_tile_kernel<ST, TF, NF><<<dim3(static_cast<unsigned>((blocks + 7) / 8 * 8)), dim3(kGateTileWaves * 64), G::kLdsBytes, stream>>>(
+            x + t0 * s.d_model, wg, bias, logits + t0 * s.E, tokens, s.d_model, s.E, groups);
+    }
     return hipGetLastError();
 }
 template <typename ST>
