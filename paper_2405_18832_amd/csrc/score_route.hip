@@ -89,8 +89,10 @@ __global__ __launch_bounds__(kGateWaves * 64) void gate_few_kernel(const ST* __r
 
 // Many tokens: 16 TF tokens x 64 NF experts per block of four wavefronts (16 NF experts each), through a ring of LDS stages of one 128-byte line of every
 // row, copied by eight consecutive lanes each, the tokens' rows first.  What follows needs rows of whole 16-byte pieces; a last line that is not whole
-// is copied with its first piece in place of those that do not exist, which are taken as zeros of both operands.  What bounds it is how much is on its way
-// from memory: 5003 x 256 x 2048 in bf16 12.8 us with six stages and a block per CU, 16.4 with four and two blocks; 16384 tokens 30 us, 2.5 TB/s of x.
+// is copied with its first piece in place of those that do not exist, which are taken as zeros of both operands.  5003 x 256 x 2048 in bf16 take 12.8 to 13.9 us
+// (16.4 with four stages, two blocks per CU and 64 tokens to a block), 16384 tokens 29.  Bound by copies out of the L2s: of the former 1.33 million lines, 170 MB, of which
+// 30 MB come from memory (x is 20 MB; the weights are copied once per block of tokens), some 17 TB/s behind the launch; matrix units busy 0.18.  In 32 bits by the
+// matrix units too, whose instructions take 32 clocks for four columns: 16384 tokens 147 us, 0.74 of their rate; a wavefront's 1024 of 1024 tokens 14 of 26 us.
 constexpr int kGateTileWaves = 4, kGateStages = 6;
 template <int TF, int NF>
 struct GateTile {
@@ -782,8 +784,9 @@ __device__ __forceinline__ void finish_counts(const ScoreArgs& a, int mine, int3
 }
 
 // A block takes `tokens` tokens, 4 per wavefront at a time.  ONE: it is the only block and goes on to the outputs of the
-// counts; else its counts go to the workspace, [block][E] of 16 bits.  Bound by vector instructions (1172 per four tokens of 256 experts, which sort a lane's
-// 16 choices and merge eight out of 16 lanes): 16384 tokens take 20 us of the 24 with the counts, all of it in 64 bits 241; one token 6.7 us.
+// counts; else its counts go to the workspace, [block][E] of 16 bits.  16384 tokens of 256 experts, k = 8, take 20 us of the 24 with the counts; all of it in 64 bits
+// 99; one token 7 us.  Of these 20 the vector units work 0.53 (1504 instructions per four tokens, the tokens in doubt with them, two wavefronts to a SIMD), beside half as
+// many scalar instructions; a wavefront waits 0.43 of its time, for the first loads, for LDS and from one round's reductions to the next's.
 template <int V>
 constexpr int kRouteScoreWaves = V <= 16 ? 8 : 4;
 template <int V, bool SIGMOID, bool BALANCED, bool ONE>
