@@ -34,7 +34,7 @@ constexpr float kTail = ACT == MOE_ACT_GELU ? -12.f : -80.f;
 constexpr float kSmallGate = 0x1p-124f, kLargeFactor = 0x1p+20f;
 constexpr float kHuge = __builtin_huge_valf();
 
-// One pass, the row in registers from the largest value to the codes.  Bound by memory: gated SiLU of 20011 x 2048 in bf16 45.3 to 46.4 us, 4.5 TB/s read + written (a
+// One pass, the row in registers from the largest value to the codes.  Bound by memory: gated SiLU of 20011 x 2048 in bf16 44.8 to 46.4 us, 4.5 TB/s read + written (a
 // copy reaches 5.1; 44.6 with a divisor whose error was not counted, 47 with what fp32 does not hold looked for in the same pass); 64 x 8192 6.9 us, of which a launch is 3.5.
 template <typename ST, int ACT, bool GATED, int WPR, int WAVES, int NV>
 __global__ __launch_bounds__(WAVES * 64) void act_int_kernel(const IntRowArgs a) {
